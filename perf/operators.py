@@ -134,15 +134,14 @@ def _normal(g, c, *shape):
 
 
 def _pool(g, c, layers, pages):
-    """K and V pages of every layer: [layers][2][pages][heads][rows of a page][d], and a tensor per layer as a decoder
-    holds them."""
+    """K and V pages of every layer: [layers][2][pages][heads][rows of a page][d]; K and V of them."""
     kv = _normal(g, c, layers, 2, pages, c["hkv"], c["page_rows"], c["d"])
-    return kv, list(kv[:, 0].unbind(0)), list(kv[:, 1].unbind(0))
+    return kv, kv[:, 0], kv[:, 1]
 
 
 def _planes(g, c, layers, rows):
     kv = _normal(g, c, layers, 2, c["hkv"], rows, c["d"])
-    return kv, list(kv[:, 0].unbind(0)), list(kv[:, 1].unbind(0))
+    return kv, kv[:, 0], kv[:, 1]
 
 
 def _table(pages, counts):
