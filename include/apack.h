@@ -16,6 +16,15 @@
  *   apack_prefill_flops   analytic prefill FLOPs of a token-length schedule
  *                         (Appendix G)
  *
+ * and what a decoder does before and after a prune:
+ *
+ *   apack_rotary          rotary positions of queries and keys
+ *   apack_compact_kv_pages  the kept rows into, out of and between pages of a
+ *                         paged cache
+ *   apack_pages_*         allocation, forking, freeing and copying of pages
+ *   apack_rotary_append   a decode step's new tokens: turned and appended
+ *   apack_paged_attention a decode step's attention over a paged cache
+ *
  * Conventions shared by every entry point
  * ---------------------------------------
  * - Tensor arguments are DEVICE pointers on the current HIP device.
@@ -388,6 +397,224 @@ apack_status apack_score_dynamics(int32_t n_seq, const apack_av_seq* seqs, apack
                                   int32_t* kept_visual, int64_t kept_capacity,
                                   int64_t* n_kept_visual,
                                   void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* Rotary positions                                                         */
+/* ------------------------------------------------------------------------ */
+
+#define APACK_ROPE_MAX_PAIRS 128
+
+/* Which elements of a head's first rot_dim make pair i < rot_dim/2. */
+#define APACK_ROPE_HALF 0         /* (i, i + rot_dim/2)                       */
+#define APACK_ROPE_INTERLEAVED 1  /* (2i, 2i + 1)                             */
+
+/* Frequencies f_i = base^(-2i/rot_dim) of pair i, and how they are scaled for
+ * contexts longer than the trained_len rows that a model was trained on, by a
+ * factor s >= 1:
+ *   NONE      f_i
+ *   LINEAR    f_i / s
+ *   NTK       base s^(rot_dim/(rot_dim-2)) in the place of base
+ *   BY_PARTS  (1-g) f_i/s + g f_i with g = clamp((t_i - 1)/(32 - 1), 0, 1)
+ *             and t_i = trained_len f_i / 2 pi turns over the trained length;
+ *             the turned elements are multiplied by 0.1 ln s + 1 */
+#define APACK_ROPE_SCALE_NONE 0
+#define APACK_ROPE_SCALE_LINEAR 1
+#define APACK_ROPE_SCALE_NTK 2
+#define APACK_ROPE_SCALE_BY_PARTS 3
+
+typedef struct apack_rope {
+  int32_t rot_dim;      /* elements of a head that turn: even, 2 to 256       */
+  int32_t layout;       /* APACK_ROPE_HALF or APACK_ROPE_INTERLEAVED          */
+  int32_t pos_rows;     /* rows of position ids (1 to 4; 3 for TMRoPE ids)    */
+  int32_t transpose;    /* 1: turn the other way (see apack_rotary)           */
+  int32_t sections[4];  /* pairs that each position row turns, in pair order;
+                         * their sum over pos_rows is rot_dim/2               */
+  double factor;        /* the turned elements are multiplied by it           */
+  double freq[APACK_ROPE_MAX_PAIRS];  /* radians per position of pair i       */
+} apack_rope;
+
+/* Fills r for one row of position ids, with freq and factor as above; the
+ * caller may then set pos_rows and sections, transpose, or frequencies of its
+ * own.  base > 1; s (>= 1) and trained_len (>= 1) are read only by the scalings
+ * that use them; NTK needs rot_dim > 2. */
+apack_status apack_rope_init(apack_rope* r, int32_t rot_dim, int32_t layout, double base,
+                             int32_t scaling, double s, int64_t trained_len);
+
+/* A [heads][rows][d] tensor with any order of heads and rows: element e of row
+ * r of head h lies at data + h*head_stride + r*row_stride + e (elements). */
+typedef struct apack_heads {
+  void* data;
+  int32_t heads;
+  int32_t reserved;     /* must be 0 */
+  int64_t head_stride;
+  int64_t row_stride;
+} apack_heads;
+
+/* Turns pair (a, b) of every row of q and k by theta = pos * freq:
+ *   a' = factor (a cos theta - b sin theta),  b' = factor (a sin theta + b cos theta)
+ * with the row of position ids that the pair's section names; elements from
+ * rot_dim on are copied.  With transpose, sin changes its sign: the gradient
+ * of the call without it with respect to its input, given that of its output,
+ * and with factor 1 the inverse.  Angles are formed in fp64 and reduced to one
+ * turn before the sine and cosine, so far positions lose nothing; products and
+ * sums are fp32, rounded once.
+ *
+ *   pos   DEVICE int32 [pos_rows][rows], row stride pos_stride; any value.
+ *   q_in/q_out, k_in/k_out: either pair may be NULL; heads and strides as
+ *   given, d <= 512, rot_dim <= d.  An output may be its own input (the same
+ *   data and strides); otherwise it overlaps no input, no other output and not
+ *   pos (APACK_E_ALIAS).  Inputs and outputs may be slices of one tensor whose
+ *   elements interleave, as of a fused projection.
+ */
+apack_status apack_rotary(const apack_rope* rope, int64_t rows, const int32_t* pos,
+                          int64_t pos_stride, apack_dtype dtype, int32_t d,
+                          const apack_heads* q_in, const apack_heads* q_out,
+                          const apack_heads* k_in, const apack_heads* k_out, void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* A cache of pages                                                         */
+/* ------------------------------------------------------------------------ */
+
+/* The K and V of n_layers layers in a pool of pages of page_rows rows each,
+ * and the pages of each sequence: row j of sequence s lies in page
+ * table[s][j / page_rows], at row j % page_rows of it.  Element e of row r of
+ * head h of page p of layer l lies at
+ *   k[l] + p*page_stride + h*head_stride + r*row_stride + e   (elements)
+ * (v likewise), in any order of pages, heads and rows.  Page ids are shared by
+ * the layers.  A table entry outside [0, n_pages) is no page: nothing is read
+ * or written there.
+ *
+ * Without a table (NULL) the rows of all sequences are packed in one page:
+ * n_pages is 1, page_rows the rows of the planes, and rows are packed rows, as
+ * in apack_prune_layer's K.  That is how contiguous planes [hkv][rows][d] are
+ * passed: head_stride theirs, row_stride d. */
+typedef struct apack_pages {
+  int32_t n_layers;           /* 1 to 64                                      */
+  int32_t n_pages;            /* pages of the pool (>= 1)                     */
+  int32_t page_rows;          /* rows of a page (>= 1)                        */
+  int32_t hkv;                /* key heads                                    */
+  int32_t d;                  /* elements of a row                            */
+  int32_t table_width;        /* entries of a sequence's row of the table     */
+  apack_dtype dtype;
+  int32_t reserved;           /* must be 0                                    */
+  int64_t page_stride;
+  int64_t head_stride;
+  int64_t row_stride;
+  void* const* k;             /* HOST array of n_layers DEVICE pointers       */
+  void* const* v;             /* the same, or NULL: only K planes (moves)     */
+  const int32_t* table;       /* DEVICE [sequences][table_width], or NULL     */
+  int64_t table_stride;       /* >= table_width                               */
+} apack_pages;
+
+/* Bookkeeping of a pool, on the HOST: refs [n_pages] counts the tables that
+ * hold each page, 0 for a free one.  On error nothing changes.
+ *
+ * alloc  takes the n lowest free pages (refs 0 -> 1) and lists them ascending;
+ *        APACK_E_SHAPE when fewer are free.
+ * free   gives up one reference to each of n pages; every one must be held
+ *        (as often as it is listed).
+ * fork   gives n_children sequences the first n_rows rows of a parent whose
+ *        pages are `parent` (ceil(n_rows/page_rows) of them): whole pages are
+ *        shared (one reference more each), and each child gets a page of its
+ *        own, the lowest free ones in the children's order, in the place of a
+ *        last page that is not full.  children [n_children][ceil(n_rows/page_rows)]
+ *        lists their pages; copies [n_children][2] the (parent page, child page)
+ *        pairs that apack_pages_copy then has to copy, *n_copies of them
+ *        (n_children, or 0 when the last page is full). */
+apack_status apack_pages_alloc(int32_t n_pages, int32_t* refs, int64_t n, int32_t* pages);
+apack_status apack_pages_free(int32_t n_pages, int32_t* refs, int64_t n, const int32_t* pages);
+apack_status apack_pages_fork(int32_t n_pages, int32_t* refs, int32_t page_rows, int64_t n_rows,
+                              const int32_t* parent, int32_t n_children, int32_t* children,
+                              int32_t* copies, int64_t* n_copies);
+
+/* Copies pages within a pool: page pairs[i][1] of every layer's K and V becomes
+ * page pairs[i][0], on raw bits, for i < n_pairs.  pairs is a DEVICE int32
+ * [n_pairs][2] array; a pair with an id outside [0, n_pages) copies nothing.
+ * Pages written must be distinct and not among those read (otherwise the call
+ * stays inside the pool, and their contents are unspecified).  The table of
+ * `pages` is not read. */
+apack_status apack_pages_copy(const apack_pages* pages, int64_t n_pairs, const int32_t* pairs,
+                              void* stream);
+
+/* One sequence's part of apack_compact_kv_pages. */
+typedef struct apack_move {
+  int64_t src_off;   /* packed row of the sequence's first row                 */
+  int64_t n_in;      /* its rows                                               */
+  int64_t dst_off;   /* first row written: of the sequence in pages, a packed
+                      * row in planes                                          */
+  int64_t n_out;     /* rows that it keeps                                     */
+} apack_move;
+
+/* Gathers rows like apack_compact_kv, from pages or planes into pages or
+ * planes: for each sequence s in order, on raw bits and in every layer,
+ *   out row dst_off + i = in row src_rows[b_s + i] - src_off   (i < n_out)
+ * with b_s the n_out of the sequences before it.  Without a table on the input
+ * side, the input row is the packed row src_rows[b_s + i] itself.  src_rows is
+ * a DEVICE int32 array of sum n_out packed rows (apack_prune_layer's
+ * kept_rows), or NULL: then every sequence moves its first n_out <= n_in rows
+ * (planes into pages after a prefill; pages into planes).
+ *
+ * A row outside its sequence's [src_off, src_off + n_in), a source or
+ * destination row beyond its table or planes, and a row whose page is not in
+ * the pool are not copied.  in and out agree in layers, heads, d, dtype and
+ * whether there is a v.  Rows written by the call must be distinct.  in and out
+ * may be the same pool (the same k, v and strides) under two tables: the pages
+ * written must not be among those read (otherwise the call stays inside the
+ * pool, and the contents of pages written are unspecified); any other overlap
+ * is APACK_E_ALIAS. */
+apack_status apack_compact_kv_pages(int32_t n_seq, const apack_move* seqs, const int32_t* src_rows,
+                                    const apack_pages* in, const apack_pages* out, void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* Decoding over a paged cache                                              */
+/* ------------------------------------------------------------------------ */
+
+/* One new token of each of n_seq sequences: turns its q and k as apack_rotary
+ * does (q_in and q_out [hq][n_seq][d], k and v [hkv][n_seq][d], pos
+ * [pos_rows][n_seq]) and writes k and v as row lens[s] - 1 of sequence s in
+ * layer 0 of `pages` (one layer, with v and a table of n_seq rows).  lens is a
+ * DEVICE int32 [n_seq] array of the lengths that include the new token.  A
+ * sequence whose row is negative, beyond the table or in no page writes no k
+ * and v; its q is turned.  Sequences must not share the page that they write
+ * to.  q_out may be q_in; otherwise outputs overlap no inputs
+ * (APACK_E_ALIAS). */
+apack_status apack_rotary_append(const apack_rope* rope, int64_t n_seq, const int32_t* pos,
+                                 int64_t pos_stride, const int32_t* lens, const apack_heads* q_in,
+                                 const apack_heads* q_out, const apack_heads* k,
+                                 const apack_heads* v, const apack_pages* pages, void* stream);
+
+/* Workspace bytes of apack_paged_attention for these sizes (0 for sizes that
+ * it refuses). */
+size_t apack_paged_attention_workspace(int64_t n_seq, int32_t hq, int32_t hkv, int32_t d,
+                                       int64_t max_len);
+
+/* Attention of one query row per sequence over its rows of a paged cache: for
+ * query head h, which reads key head h / (hq/hkv),
+ *   o = sum_j p_j v_j,  p = softmax_j(scale q.k_j)
+ * over the rows j in [max(0, lens[s] - window), lens[s]) (window 0: all) whose
+ * page is in the pool and whose mask is not 0.  Without such a row o is 0 and
+ * lse -inf.  Rows that are left out may hold any bits.
+ *
+ *   q, out  [hq][n_seq][d]; out overlaps neither q nor the pool.
+ *   lse     fp32 [hq][n_seq] out (nullable): ln sum_j exp(scale q.k_j), with
+ *           which attentions over disjoint rows can be joined.
+ *   pages   one layer, with v and a table of n_seq rows; d 64 or 128; every
+ *           row starts 16-byte aligned.
+ *   lens    DEVICE int32 [n_seq]; rows beyond max_len or the table are left
+ *           out, so max_len (HOST) bounds the lengths that the call can meet:
+ *           a captured call may be replayed while lens grow up to it.
+ *   mask    DEVICE uint8 [n_seq][max_len] (nullable), row stride mask_stride.
+ *   scale   > 0, or 0 for 1/sqrt(d).
+ *
+ * Several new tokens of one sequence are passed as sequences with equal table
+ * rows and their own lens.  Logits, the softmax and the sums are fp32; with
+ * bf16 tensors the probabilities are rounded to bf16 for their product with V.
+ * Results do not depend on timing: the same call gives the same bits. */
+apack_status apack_paged_attention(int64_t n_seq, int32_t hq, const apack_heads* q,
+                                   const apack_heads* out, float* lse, const apack_pages* pages,
+                                   const int32_t* lens, int64_t max_len, const uint8_t* mask,
+                                   int64_t mask_stride, int64_t window, double scale,
+                                   void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

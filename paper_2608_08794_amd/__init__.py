@@ -8,6 +8,19 @@ the first call loads ``libapack.so`` next to this file and raises
 :class:`ApackError` if it is missing (build it with ``build.build()``).
 """
 
+from ._decode import (  # noqa: F401
+    Rope,
+    apack_compact_kv_pages,
+    apack_paged_attention,
+    apack_paged_attention_workspace,
+    apack_pages_alloc,
+    apack_pages_copy,
+    apack_pages_fork,
+    apack_pages_free,
+    apack_rope,
+    apack_rotary,
+    apack_rotary_append,
+)
 from ._lib import (  # noqa: F401
     APACK_AUDIO,
     APACK_BF16,
