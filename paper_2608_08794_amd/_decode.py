@@ -1,11 +1,10 @@
 """ctypes binding of the rotary, paged-cache and decode calls of include/apack.h
 (argument marshalling only)."""
 
-import contextlib
 import ctypes
 
 from . import _lib
-from ._lib import ApackError, _alloc_on, _check, _stream, _torch, _workspace, library
+from ._lib import ApackError, _alloc_on, _check, _torch, library
 
 ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
 ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "by_parts": 3}
@@ -58,56 +57,76 @@ def _fail(status, message):
     raise ApackError(status, message)
 
 
-class _Device:
-    """The device of a call: every tensor must lie on it, and it must be the current one."""
-
-    def __init__(self):
-        self.index = None
-
-    def take(self, t, name, dtype=None):
-        if not t.is_cuda:
-            _fail(1, f"{name} must be a CUDA tensor")
-        i = t.get_device()
-        if self.index is None:
-            self.index = i
-            if i != _torch().cuda.current_device():
-                _fail(1, f"{name} lies on device {i}, which is not the current one")
-        elif i != self.index:
-            _fail(1, f"{name} lies on device {i}, other tensors on {self.index}")
-        if dtype is not None and t.dtype != dtype:
-            _fail(3, f"{name} must be {dtype}, not {t.dtype}")
-        return t.data_ptr()
+def _on_device(*named):
+    """The device that every (tensor, name) lies on; it must be the current one."""
+    torch = _torch()
+    index = named[0][0].get_device()
+    for t, name in named:
+        if t.get_device() != index or index < 0:
+            _fail(1, f"{name} must be a CUDA tensor on the call's device")
+    if index != torch.cuda.current_device():
+        _fail(1, f"the tensors lie on device {index}, which is not the current one")
+    return index
 
 
-def _heads(dev, t, name, dtype):
+def _stream_on(stream, index):
+    """The stream's handle: the given one, or the device's current one."""
+    if stream is None:
+        return _torch()._C._cuda_getCurrentRawStream(index)
+    return stream if isinstance(stream, int) else stream.cuda_stream
+
+
+def _heads(t, name, dtype):
     """[heads, rows, d] with contiguous elements and any order of heads and rows."""
-    p = dev.take(t, name, dtype)
+    if t.dtype is not dtype:
+        _fail(3, f"{name} must be {dtype}, not {t.dtype}")
     if t.dim() != 3:
         _fail(2, f"{name} must be [heads, rows, d]")
     sh, sr, se = t.stride()
     if se != 1 and t.shape[2] > 1:
         _fail(2, f"{name} must have contiguous elements")
-    return Heads(p, t.shape[0], 0, sh, sr)
+    return Heads(t.data_ptr(), t.shape[0], 0, sh, sr)
 
 
-def _layers(dev, x, dims, name):
-    """(pointers, shape, strides, dtype) of a tensor per layer: a list of them, or one tensor whose first dimension is
-    the layer."""
+def _int32(t, name, dims):
+    """A contiguous int32 tensor."""
+    if t.dtype is not _torch().int32:
+        _fail(3, f"{name} must be int32, not {t.dtype}")
+    if t.dim() != dims or not t.is_contiguous():
+        _fail(2, f"{name} must be contiguous, of {dims} dimension{'s' if dims > 1 else ''}")
+    return t.data_ptr()
+
+
+def _first(x, name):
+    """One of the tensors of a list of layers, or of one tensor of them all."""
     if isinstance(x, (list, tuple)):
         if not x:
             _fail(1, f"{name} needs one tensor per layer")
-        first = x[0]
-        shape, stride, dtype = first.shape, first.stride(), first.dtype
-        ptrs = [dev.take(t, name, dtype) for t in x]
-        if any(t.shape != shape or t.stride() != stride for t in x):
-            _fail(2, f"the layers of {name} differ in shape or strides")
+        return x[0]
+    return x
+
+
+def _layers(x, dims, name):
+    """(pointers, shape, strides, dtype) of a tensor per layer: a list of them, or one tensor whose first dimension is
+    the layer."""
+    if isinstance(x, (list, tuple)):
+        first = _first(x, name)
+        shape, stride, dtype, index = first.shape, first.stride(), first.dtype, first.get_device()
+        ptrs = []
+        for t in x:
+            if t.shape != shape or t.stride() != stride:
+                _fail(2, f"the layers of {name} differ in shape or strides")
+            if t.dtype is not dtype or t.get_device() != index:
+                _fail(3, f"the layers of {name} differ in dtype or device")
+            ptrs.append(t.data_ptr())
     else:
-        base = dev.take(x, name)
+        base, n = x.data_ptr(), x.shape[0]
         if x.dim() != dims + 1:
             _fail(2, f"{name} must be a list of layers or one tensor [layers, ...] of {dims + 1} dimensions")
-        shape, stride, dtype = x.shape[1:], x.stride()[1:], x.dtype
-        step = x.stride(0) * x.element_size()
-        ptrs = [base + i * step for i in range(x.shape[0])]
+        shape, stride, dtype = x.shape[1:], x.stride(), x.dtype
+        step = stride[0] * x.element_size()
+        ptrs = range(base, base + n * step, step) if step > 0 else [base] * n
+        stride = stride[1:]
     if len(shape) != dims:
         _fail(2, f"the layers of {name} must have {dims} dimensions")
     if stride[-1] != 1 and shape[-1] > 1:
@@ -115,66 +134,69 @@ def _layers(dev, x, dims, name):
     return ptrs, shape, stride, dtype
 
 
-def _table(dev, t, n_seq):
-    p = dev.take(t, "table", _torch().int32)
-    if t.dim() != 2 or t.shape[0] != n_seq:
-        _fail(2, f"table must be [{n_seq}, pages]")
-    if t.stride(1) != 1 and t.shape[1] > 1:
-        _fail(2, "table must have contiguous rows")
-    return p, t.shape[1], max(t.stride(0), t.shape[1]) if n_seq < 2 else t.stride(0)
-
-
-def _pages(dev, k, v, table=None, n_seq=0, name="pages", planes=False):
+def _pages(k, v, table=None, n_seq=0, name="pages", planes=False):
     """An apack_pages of [pages, heads, rows, d] tensors, or of planes [heads, rows, d]."""
     dims = 3 if planes else 4
-    ptrs, shape, stride, dtype = _layers(dev, k, dims, f"k_{name}")
+    ptrs, shape, stride, dtype = _layers(k, dims, f"k_{name}")
     n = len(ptrs)
-    p = Pages()
-    p.n_layers, p.dtype = n, _code(dtype)
-    p.k = (_P * n)(*ptrs)
+    kp, vp = (_P * n)(*ptrs), None
     if v is not None and len(v):
-        vp, vshape, vstride, vdtype = _layers(dev, v, dims, f"v_{name}")
-        if len(vp) != n or vshape != shape or vstride != stride:
+        ptrs, vshape, vstride, vdtype = _layers(v, dims, f"v_{name}")
+        if len(ptrs) != n or vshape != shape or vstride != stride:
             _fail(2, f"v_{name} must match k_{name} in layers, shape and strides")
-        if vdtype != dtype:
+        if vdtype is not dtype:
             _fail(3, f"v_{name} must match k_{name} in dtype")
-        p.v = (_P * n)(*vp)
+        vp = (_P * n)(*ptrs)
     if planes:
-        p.n_pages, p.hkv, p.page_rows, p.d = 1, shape[0], shape[1], shape[2]
-        p.head_stride, p.row_stride = stride[0], stride[1]
+        pages, (hkv, rows, d), (sh, sr, _), sp = 1, shape, stride, 0
     else:
-        p.n_pages, p.hkv, p.page_rows, p.d = shape
-        p.page_stride, p.head_stride, p.row_stride = stride[0], stride[1], stride[2]
+        (pages, hkv, rows, d), (sp, sh, sr, _) = shape, stride
+    tp, width, ts = None, 0, 0
     if table is not None:
-        p.table, p.table_width, p.table_stride = _table(dev, table, n_seq)
-    return p
+        if table.dtype is not _torch().int32:
+            _fail(3, f"the table must be int32, not {table.dtype}")
+        if table.dim() != 2 or table.shape[0] != n_seq:
+            _fail(2, f"the table must be [{n_seq}, pages]")
+        width = table.shape[1]
+        ts, se = table.stride()
+        if se != 1 and width > 1:
+            _fail(2, "the table must have contiguous rows")
+        tp, ts = table.data_ptr(), ts if n_seq > 1 else width
+    return Pages(n, pages, rows, hkv, d, width, _code(dtype), 0, sp, sh, sr, kp, vp, tp, ts)
 
 
 def _code(dtype):
     torch = _torch()
-    if dtype == torch.bfloat16:
+    if dtype is torch.bfloat16:
         return _lib.APACK_BF16
-    if dtype == torch.float32:
+    if dtype is torch.float32:
         return _lib.APACK_F32
     _fail(3, f"unsupported dtype {dtype}")
 
 
-def _on(stream):
-    return contextlib.nullcontext() if stream is None else _alloc_on(stream)
+def _new(stream, shape, dtype, device):
+    """An output, allocated on the stream that the call runs on."""
+    torch = _torch()
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with _alloc_on(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
 
 
-def _positions(dev, pos, rope, rows):
+def _positions(pos, rope, rows):
     """(pointer, row stride) of position ids [rows] or [pos_rows, rows]."""
-    p = dev.take(pos, "pos", _torch().int32)
-    shape = tuple(pos.shape)
-    if shape != (rope.pos_rows, rows) and not (rope.pos_rows == 1 and shape == (rows,)):
-        _fail(2, f"pos must be [{rope.pos_rows}, {rows}]")
-    if rows > 1 and pos.stride(-1) != 1:
+    if pos.dtype is not _torch().int32:
+        _fail(3, f"pos must be int32, not {pos.dtype}")
+    n, shape = rope.pos_rows, pos.shape
+    if shape != (n, rows) and not (n == 1 and shape == (rows,)):
+        _fail(2, f"pos must be [{n}, {rows}]")
+    stride = pos.stride()
+    if rows > 1 and stride[-1] != 1:
         _fail(2, "pos must have contiguous rows")
-    return p, pos.stride(0) if rope.pos_rows > 1 else rows
+    return pos.data_ptr(), stride[0] if n > 1 else rows
 
 
-def _int32_cpu(t, name, shape=None):
+def _int32_cpu(t, name):
     """A contiguous int32 tensor in host memory (bookkeeping)."""
     torch = _torch()
     if not isinstance(t, torch.Tensor) or t.is_cuda or t.dtype != torch.int32 or not t.is_contiguous():
@@ -215,41 +237,41 @@ def apack_rotary(pos, rope, q=None, k=None, q_out=None, k_out=None, transpose=No
     [heads, rows, d] tensors.  transpose (rope's by default) turns the other
     way: the gradient of the call, and with factor 1 its inverse.  Returns
     (q_out, k_out)."""
-    torch = _torch()
-    dev = _Device()
     some = q if q is not None else k
     if some is None:
         _fail(1, "neither q nor k")
-    if some.dim() != 3:
-        _fail(2, "q and k must be [heads, rows, d]")
-    if k is not None and (k.dim() != 3 or k.shape[1:] != some.shape[1:]):
-        _fail(2, "q and k must agree in rows and d")
     if (q is None and q_out is not None) or (k is None and k_out is not None):
         _fail(1, "an output without its input")
+    if some.dim() != 3:
+        _fail(2, "q and k must be [heads, rows, d]")
+    index = _on_device((pos, "pos"), *[(t, n) for t, n in ((q, "q"), (k, "k"), (q_out, "q_out"), (k_out, "k_out"))
+                                       if t is not None])
     if transpose is not None and bool(transpose) != bool(rope.transpose):
         rope = Rope.from_buffer_copy(rope)
         rope.transpose = 1 if transpose else 0
     _, rows, d = some.shape
-    p, ps = _positions(dev, pos, rope, rows)
     dtype = some.dtype
     code = _code(dtype)
-    pairs = []
-    outs = []
-    for x, y, name in ((q, q_out, "q"), (k, k_out, "k")):
-        if x is None:
-            pairs += [None, None]
-            outs.append(None)
-            continue
-        hx = _heads(dev, x, name, dtype)
-        if y is None:
-            with _on(stream):
-                y = torch.empty(x.shape, dtype=dtype, device=x.device)
-        elif y.shape != x.shape:
-            _fail(2, f"{name}_out must have {name}'s shape")
-        pairs += [hx, _heads(dev, y, name + "_out", dtype)]
-        outs.append(y)
-    _check(library().apack_rotary(rope, rows, p, ps, code, d, *pairs, _stream(stream)))
-    return outs[0], outs[1]
+    p, ps = _positions(pos, rope, rows)
+    hq = hk = hqo = hko = None
+    if q is not None:
+        hq = _heads(q, "q", dtype)
+        if q_out is None:
+            q_out = _new(stream, q.shape, dtype, q.device)
+        elif q_out.shape != q.shape:
+            _fail(2, "q_out must have q's shape")
+        hqo = _heads(q_out, "q_out", dtype)
+    if k is not None:
+        hk = _heads(k, "k", dtype)
+        if k.shape[1:] != some.shape[1:]:
+            _fail(2, "q and k must agree in rows and d")
+        if k_out is None:
+            k_out = _new(stream, k.shape, dtype, k.device)
+        elif k_out.shape != k.shape:
+            _fail(2, "k_out must have k's shape")
+        hko = _heads(k_out, "k_out", dtype)
+    _check(library().apack_rotary(rope, rows, p, ps, code, d, hq, hqo, hk, hko, _stream_on(stream, index)))
+    return q_out, k_out
 
 
 def apack_pages_alloc(refs, n):
@@ -289,11 +311,12 @@ def apack_pages_copy(pairs, k_pages, v_pages=(), stream=None):
     """Copies page pairs[i, 0] to page pairs[i, 1] in every layer's K and V.
     pairs: int32 CUDA tensor [n, 2]; k_pages, v_pages: per layer [pages, heads,
     rows, d], or one tensor [layers, pages, heads, rows, d]."""
-    dev = _Device()
-    p = dev.take(pairs, "pairs", _torch().int32)
-    if pairs.dim() != 2 or pairs.shape[1] != 2 or not pairs.is_contiguous():
-        _fail(2, "pairs must be a contiguous [n, 2] tensor")
-    _check(library().apack_pages_copy(_pages(dev, k_pages, v_pages), pairs.shape[0], p, _stream(stream)))
+    index = _on_device((pairs, "pairs"), (_first(k_pages, "k_pages"), "k_pages"),
+                       *([(_first(v_pages, "v_pages"), "v_pages")] if len(v_pages) else []))
+    p = _int32(pairs, "pairs", 2)
+    if pairs.shape[1] != 2:
+        _fail(2, "pairs must be [n, 2]")
+    _check(library().apack_pages_copy(_pages(k_pages, v_pages), pairs.shape[0], p, _stream_on(stream, index)))
 
 
 def apack_compact_kv_pages(src_rows, seqs, k_in, v_in, k_out, v_out, table_in=None, table_out=None, stream=None):
@@ -305,18 +328,24 @@ def apack_compact_kv_pages(src_rows, seqs, k_in, v_in, k_out, v_out, table_in=No
     (src_off, n_in, dst_off, n_out) per sequence.  With a table [n_seq, pages]
     a side's tensors are [pages, heads, rows, d] per layer, without one [heads,
     rows, d]; a list of layers or one tensor with layers first."""
-    torch = _torch()
-    dev = _Device()
     n = len(seqs)
+    used = [(_first(k_in, "k_in"), "k_in"), (_first(k_out, "k_out"), "k_out")]
+    for x, name in ((v_in, "v_in"), (v_out, "v_out")):
+        if len(x):
+            used.append((_first(x, name), name))
+    for x, name in ((src_rows, "src_rows"), (table_in, "table_in"), (table_out, "table_out")):
+        if x is not None:
+            used.append((x, name))
+    index = _on_device(*used)
     moves = (Move * max(1, n))(*seqs)
     src = None
     if src_rows is not None:
-        src = dev.take(src_rows, "src_rows", torch.int32)
-        if src_rows.numel() != sum(m[3] for m in seqs) or not src_rows.is_contiguous():
-            _fail(2, "src_rows must be contiguous, with sum n_out rows")
-    pin = _pages(dev, k_in, v_in, table_in, n, "in", planes=table_in is None)
-    pout = _pages(dev, k_out, v_out, table_out, n, "out", planes=table_out is None)
-    _check(library().apack_compact_kv_pages(n, moves, src, pin, pout, _stream(stream)))
+        src = _int32(src_rows, "src_rows", 1)
+        if src_rows.shape[0] != sum([m[3] for m in seqs]):
+            _fail(2, "src_rows must hold sum n_out rows")
+    pin = _pages(k_in, v_in, table_in, n, "in", planes=table_in is None)
+    pout = _pages(k_out, v_out, table_out, n, "out", planes=table_out is None)
+    _check(library().apack_compact_kv_pages(n, moves, src, pin, pout, _stream_on(stream, index)))
 
 
 def apack_rotary_append(pos, rope, q, k, v, k_pages, v_pages, table, lens, q_out=None, stream=None):
@@ -324,32 +353,31 @@ def apack_rotary_append(pos, rope, q, k, v, k_pages, v_pages, table, lens, q_out
     k [hkv, n_seq, d] and writes k and v [hkv, n_seq, d] as row lens[s] - 1 of
     sequence s into one layer's pages [pages, hkv, rows, d].  Returns q_out (new
     if not given; it may be q)."""
-    torch = _torch()
-    dev = _Device()
     if q.dim() != 3:
         _fail(2, "q must be [hq, n_seq, d]")
-    n, dtype = q.shape[1], q.dtype
-    p, ps = _positions(dev, pos, rope, n)
-    hq = _heads(dev, q, "q", dtype)
-    pages = _pages(dev, [k_pages], [v_pages], table, n)
-    if pages.dtype != _code(dtype):
+    index = _on_device((q, "q"), (pos, "pos"), (k, "k"), (v, "v"), (k_pages, "k_pages"), (v_pages, "v_pages"),
+                       (table, "table"), (lens, "lens"), (q if q_out is None else q_out, "q_out"))
+    _, n, d = q.shape
+    dtype = q.dtype
+    p, ps = _positions(pos, rope, n)
+    pages = _pages((k_pages,), (v_pages,), table, n)
+    hq, hk, hv = _heads(q, "q", dtype), _heads(k, "k", dtype), _heads(v, "v", dtype)
+    if k_pages.dtype is not dtype:
         _fail(3, "q and the pages must share a dtype")
-    for x, name in ((k, "k"), (v, "v")):
-        if tuple(x.shape) != (pages.hkv, n, pages.d):
-            _fail(2, f"{name} must be [{pages.hkv}, {n}, {pages.d}]")
-    if q.shape[2] != pages.d:
+    if d != pages.d:
         _fail(2, "q and the pages differ in d")
-    lp = dev.take(lens, "lens", torch.int32)
-    if lens.shape != (n,) or not lens.is_contiguous():
-        _fail(2, f"lens must be a contiguous [{n}] tensor")
-    hk, hv = _heads(dev, k, "k", dtype), _heads(dev, v, "v", dtype)
+    shape = (pages.hkv, n, d)
+    if k.shape != shape or v.shape != shape:
+        _fail(2, f"k and v must be [{pages.hkv}, {n}, {d}]")
+    lp = _int32(lens, "lens", 1)
+    if lens.shape[0] != n:
+        _fail(2, f"lens must be [{n}]")
     if q_out is None:
-        with _on(stream):
-            q_out = torch.empty(q.shape, dtype=dtype, device=q.device)
+        q_out = _new(stream, q.shape, dtype, q.device)
     elif q_out.shape != q.shape:
         _fail(2, "q_out must have q's shape")
-    _check(library().apack_rotary_append(rope, n, p, ps, lp, hq, _heads(dev, q_out, "q_out", dtype), hk, hv, pages,
-                                         _stream(stream)))
+    _check(library().apack_rotary_append(rope, n, p, ps, lp, hq, _heads(q_out, "q_out", dtype), hk, hv, pages,
+                                         _stream_on(stream, index)))
     return q_out
 
 
@@ -366,46 +394,49 @@ def apack_paged_attention(q, k_pages, v_pages, table, lens, max_len, mask=None, 
     rows (0: all); scale: 1/sqrt(d) by default.  Returns out [hq, n_seq, d] (new
     if not given), and with return_lse (out, lse [hq, n_seq] fp32)."""
     torch = _torch()
-    dev = _Device()
     if q.dim() != 3:
         _fail(2, "q must be [hq, n_seq, d]")
+    index = _on_device((q, "q"), (k_pages, "k_pages"), (v_pages, "v_pages"), (table, "table"), (lens, "lens"),
+                       *[(t, n) for t, n in ((mask, "mask"), (out, "out"), (lse, "lse"), (workspace, "workspace"))
+                         if t is not None])
     hq, n, d = q.shape
     dtype, max_len = q.dtype, int(max_len)
-    qh = _heads(dev, q, "q", dtype)
-    pages = _pages(dev, [k_pages], [v_pages], table, n)
-    if pages.dtype != _code(dtype):
+    qh = _heads(q, "q", dtype)
+    pages = _pages((k_pages,), (v_pages,), table, n)
+    if k_pages.dtype is not dtype:
         _fail(3, "q and the pages must share a dtype")
     if d != pages.d:
         _fail(2, "q and the pages differ in d")
-    lp = dev.take(lens, "lens", torch.int32)
-    if lens.shape != (n,) or not lens.is_contiguous():
-        _fail(2, f"lens must be a contiguous [{n}] tensor")
-    mp = ms = 0
+    lp = _int32(lens, "lens", 1)
+    if lens.shape[0] != n:
+        _fail(2, f"lens must be [{n}]")
+    mp, ms = None, 0
     if mask is not None:
-        mp = dev.take(mask, "mask")
         if mask.dtype not in (torch.bool, torch.uint8):
             _fail(3, "mask must be bool or uint8")
-        if tuple(mask.shape) != (n, max_len) or (max_len > 1 and mask.stride(1) != 1):
+        if mask.shape != (n, max_len) or (max_len > 1 and mask.stride(1) != 1):
             _fail(2, f"mask must be [{n}, {max_len}] with contiguous rows")
-        ms = mask.stride(0) if n > 1 else max_len
+        mp, ms = mask.data_ptr(), mask.stride(0) if n > 1 else max_len
     if scale is not None and not scale > 0:
         _fail(1, "scale must be > 0")
-    with _on(stream):
-        if out is None:
-            out = torch.empty(q.shape, dtype=dtype, device=q.device)
-        if return_lse and lse is None:
-            lse = torch.empty((hq, n), dtype=torch.float32, device=q.device)
-        if workspace is None:
-            workspace = _workspace(library().apack_paged_attention_workspace(n, hq, pages.hkv, d, max_len), q.device)
-    if out.shape != q.shape:
+    if out is None:
+        out = _new(stream, q.shape, dtype, q.device)
+    elif out.shape != q.shape:
         _fail(2, "out must have q's shape")
+    if return_lse and lse is None:
+        lse = _new(stream, (hq, n), torch.float32, q.device)
     sp = None
     if lse is not None:
-        sp = dev.take(lse, "lse", torch.float32)
-        if tuple(lse.shape) != (hq, n) or not lse.is_contiguous():
+        if lse.dtype is not torch.float32:
+            _fail(3, "lse must be float32")
+        if lse.shape != (hq, n) or not lse.is_contiguous():
             _fail(2, f"lse must be a contiguous [{hq}, {n}] tensor")
-    wp = dev.take(workspace, "workspace", torch.uint8)
-    _check(library().apack_paged_attention(n, hq, qh, _heads(dev, out, "out", dtype), sp, pages, lp, max_len, mp, ms,
-                                           int(window), 0.0 if scale is None else float(scale), wp, workspace.numel(),
-                                           _stream(stream)))
+        sp = lse.data_ptr()
+    lib = library()
+    if workspace is None:
+        need = lib.apack_paged_attention_workspace(n, hq, pages.hkv, d, max_len)
+        workspace = _new(stream, (max(need, 256),), torch.uint8, q.device)
+    _check(lib.apack_paged_attention(n, hq, qh, _heads(out, "out", dtype), sp, pages, lp, max_len, mp, ms, int(window),
+                                     0.0 if scale is None else float(scale), workspace.data_ptr(),
+                                     workspace.numel() * workspace.element_size(), _stream_on(stream, index)))
     return (out, lse) if return_lse else out
