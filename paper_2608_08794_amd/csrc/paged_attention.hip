@@ -15,9 +15,10 @@
 //           whole rows, then a transpose of 16-bit values between registers.
 // Probabilities, maxima, sums and rescaling of a head all sit in its lane.
 //
-// The rows of a sequence are split over workgroups (chunks of a size that fills
-// the chip); each leaves its maximum, sum and unnormalised output, and a second
-// kernel joins them.
+// The rows of all sequences and key heads, in tiles of 32, are dealt to the
+// workgroups in equal shares, whatever the lengths on the device are.  Where a
+// share's border falls inside a sequence's key head, each side leaves its
+// maximum, sum and unnormalised output, and a second kernel joins them.
 #include <cmath>
 #include <cstring>
 
@@ -31,12 +32,13 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kWaves = 4;
-constexpr int kThreads = 64 * kWaves;
 constexpr int kHeads = 16;        // query heads of a workgroup: an MFMA's columns
-constexpr int kTile = 32;         // rows of a wave's step
-constexpr int kMinChunk = kWaves * kTile;
-constexpr int kMaxChunk = 2048;   // rows of a workgroup; its page ids lie in LDS
+constexpr int kTile = 32;         // rows of a tile
+constexpr int kChunk = 2048;      // rows whose page ids lie in LDS at a time
+constexpr int kShareWaves = 4;    // waves of a workgroup that takes a share
+constexpr int kWholeWaves = 8;    // ... that takes a sequence's key head whole
+constexpr int kShares = 768;      // three workgroups a compute unit: what the registers let run at once
+template <int D> constexpr int kPart = D + 4;   // floats of a head's part: output, maximum, sum, 16-byte aligned
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -48,16 +50,31 @@ struct AttnArgs {
   const void* v;
   const int32_t* lens;
   const uint8_t* mask;
-  float* part;                    // [seq][head][chunk][D + 2]: output, maximum, sum
+  int32_t* split;                 // [seq][item]: parts, first part's slot, first share
+  float* part;                    // [slot][head][kPart<D>]
   int64_t q_head, q_row, out_head, out_row, mask_stride;   // elements
   int64_t max_len, window;
   int64_t n_seq;
   int32_t hkv, group;             // key heads; query heads of each
   int32_t tiles;                  // ceil(group / kHeads)
-  int32_t chunk, chunks;          // rows of a workgroup; workgroups of a sequence's key head
+  int32_t shares;
   float scale;
   PoolDev pages;
 };
+
+// Rows [lo, lo + n) that a sequence attends to, and their tiles (one, of no
+// rows, when there are none, so that its output is written).
+struct Rows {
+  int64_t lo;
+  int n, tiles;
+};
+__device__ __forceinline__ Rows rows_of(const AttnArgs& a, int64_t seq) {
+  const int64_t have = a.lens[seq];
+  const int64_t len = max((int64_t)0, min(have, min(a.max_len, (int64_t)a.pages.table_width * a.pages.rows.d)));
+  const int64_t lo = a.window > 0 ? max((int64_t)0, have - a.window) : 0;
+  const int n = (int)max((int64_t)0, len - lo);
+  return {lo, n, max(1, (n + kTile - 1) / kTile)};
+}
 
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -69,6 +86,12 @@ __device__ __forceinline__ float max_of_head(float x) {
 __device__ __forceinline__ float sum_of_head(float x) {
   x += __shfl_xor(x, 16);
   return x + __shfl_xor(x, 32);
+}
+
+// K and V pass once: nontemporal loads, 6.8 TB/s where plain ones read 192 MB at 5.9.
+template <class V>
+__device__ __forceinline__ V stream(const V* p) {
+  return __builtin_nontemporal_load(p);
 }
 
 template <class T> struct Elem;
@@ -128,9 +151,7 @@ template <int D> struct Step<uint16_t, D> {
 template <int D> struct Step<float, D> {
   static constexpr int kQ = D / 16;
   static constexpr int kV = D / 16;
-  struct VRow {
-    u32x4 w[kV / 4];
-  };
+  typedef unsigned int VRow __attribute__((ext_vector_type(kV)));
   u32x4 k[1][kQ];
   VRow v[4];
 
@@ -150,240 +171,345 @@ template <int D> struct Step<float, D> {
     for (int i = 0; i < 4; ++i)
 #pragma unroll
       for (int s = 0; s < kV; ++s)
-        acc[s] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v[i].w[s / 4][s % 4]), p[i], acc[s], 0, 0, 0);
+        acc[s] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v[i][s]), p[i], acc[s], 0, 0, 0);
   }
 };
 
-template <class T, int D>
-__global__ __launch_bounds__(kThreads) void k_paged_attention(const AttnArgs a) {
+// A workgroup's state: per lane, for its head l % 16, the running maximum, its
+// keys' part of the sum, and acc[s][i], element (4 (l/16) + i) kV + s of the output.
+template <class T, int D, int kWaves>
+struct Worker {
   using S = Step<T, D>;
-  constexpr int kR = Elem<T>::kRow16, kKeys = 4 * kR, kStep = 16 * kR;
-  constexpr int kPad = D + 4;
-  __shared__ int32_t page_of[kMaxChunk + 1];
-  __shared__ float part[kWaves][kHeads][kPad];
-  __shared__ float stat[kWaves][kHeads][2];
-  __shared__ int any_bad;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int n = lane & 15, g = lane >> 4;
-  const int chunk = blockIdx.x;
-  const int kh = blockIdx.y / a.tiles, h0 = (blockIdx.y % a.tiles) * kHeads;   // key head; first head of its group
-  const int64_t seq = blockIdx.z;
-  const int heads = min(kHeads, a.group - h0);
-
-  // Rows [r0, r1) of this workgroup.
-  const uint32_t page_rows = a.pages.rows.d;
-  int64_t len = min((int64_t)a.lens[seq], min(a.max_len, (int64_t)a.pages.table_width * page_rows));
-  len = max(len, (int64_t)0);
-  const int64_t lo = a.window > 0 ? max((int64_t)0, (int64_t)a.lens[seq] - a.window) : 0;
-  const int64_t r0 = lo + (int64_t)chunk * a.chunk;
-  const int rows = (int)max((int64_t)0, min((int64_t)a.chunk, len - r0));
-  if (rows == 0 && a.chunks > 1) return;   // the join counts chunks itself
-
-  const uint32_t p0 = a.pages.rows.div((uint32_t)r0);
-  if (threadIdx.x == 0) any_bad = 0;
-  __syncthreads();
-  if (rows > 0) {
-    const int pages = (int)(a.pages.rows.div((uint32_t)(r0 + rows - 1)) - p0) + 1;
-    for (int i = threadIdx.x; i < pages; i += kThreads) {
-      int32_t p = a.pages.table[seq * a.pages.table_stride + p0 + i];
-      if (p < 0 || p >= a.pages.n_pages) {
-        p = -1;
-        any_bad = 1;
-      }
-      page_of[i] = p;
-    }
-  }
-  __syncthreads();
-  const bool holes = any_bad || a.mask;
-
-  // The query rows; heads past the group read its last one and are never stored.
-  u32x4 q[S::kQ];
-  {
-    const int h = kh * a.group + h0 + min(n, heads - 1);
-    const T* src = static_cast<const T*>(a.q) + h * a.q_head + seq * a.q_row;
-#pragma unroll
-    for (int j = 0; j < S::kQ; ++j) q[j] = *reinterpret_cast<const u32x4*>(src + S::k_off(g, j));
-  }
-  const T* kb = static_cast<const T*>(a.k) + kh * a.pages.head_stride;
-  const T* vb = static_cast<const T*>(a.v) + kh * a.pages.head_stride;
-  // Row i of the chunk, in a page (page 0 stands in where there is none).
-  auto row_at = [&](const T* base, int i) {
-    const uint32_t r = (uint32_t)(r0 + i), p = a.pages.rows.div(r);
-    return base + max(page_of[p - p0], 0) * a.pages.page_stride + (int64_t)(r - p * page_rows) * a.pages.row_stride;
+  static constexpr int kR = Elem<T>::kRow16, kKeys = 4 * kR, kStep = 16 * kR, kThreads = 64 * kWaves;
+  struct Shared {
+    int32_t page[kChunk + 1];       // ids of the pages of a chunk's rows, -1 where there is none
+    float part[kWaves][kHeads][D + 4];
+    float stat[kWaves][kHeads][2];
   };
 
-  const float c = a.scale * kLog2e;
-  float m = -INFINITY, l = 0;
-  f32x4 acc[S::kV] = {};
-  for (int i0 = wave * kStep; i0 < rows; i0 += kWaves * kStep) {
-    S st;
+  // Tiles [t0, t1) of item `item` (key head and 16 query heads) of a sequence.
+  // Writes the output, or with part != nullptr its parts.
+  static __device__ __forceinline__ void run(const AttnArgs& a, Shared& sh, int64_t seq, const Rows& of, int item, int t0,
+                                             int t1, float* part) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int n = lane & 15, g = lane >> 4;
+    const int kh = item / a.tiles, h0 = (item % a.tiles) * kHeads;
+    const int heads = min(kHeads, a.group - h0);
+    const uint32_t page_rows = a.pages.rows.d;
+
+    // The query rows; heads past the group read its last one and are never stored.
+    u32x4 q[S::kQ];
+    {
+      const int h = kh * a.group + h0 + min(n, heads - 1);
+      const T* src = static_cast<const T*>(a.q) + h * a.q_head + seq * a.q_row;
 #pragma unroll
-    for (int t = 0; t < kR; ++t) {
-      const T* src = row_at(kb, min(i0 + 16 * t + n, rows - 1));
-#pragma unroll
-      for (int j = 0; j < S::kQ; ++j) st.k[t][j] = *reinterpret_cast<const u32x4*>(src + S::k_off(g, j));
+      for (int j = 0; j < S::kQ; ++j) q[j] = *reinterpret_cast<const u32x4*>(src + S::k_off(g, j));
     }
+    const T* kb = static_cast<const T*>(a.k) + kh * a.pages.head_stride;
+    const T* vb = static_cast<const T*>(a.v) + kh * a.pages.head_stride;
+    const float c = a.scale * kLog2e;
+    float m = -INFINITY, l = 0;
+    f32x4 acc[S::kV] = {};
+
+    const int end = min(of.n, t1 * kTile);
+    for (int first = t0 * kTile; first < end; first += kChunk) {
+      const int rows = min(kChunk, end - first);
+      const int64_t r0 = of.lo + first;
+      const uint32_t p0 = a.pages.rows.div((uint32_t)r0);
+      const int pages = (int)(a.pages.rows.div((uint32_t)(r0 + rows - 1)) - p0) + 1;
+      __syncthreads();   // the last chunk's ids have been read
+      for (int i = threadIdx.x; i < pages; i += kThreads) {
+        const int32_t p = a.pages.table[seq * a.pages.table_stride + p0 + i];
+        sh.page[i] = p >= 0 && p < a.pages.n_pages ? p : -1;
+      }
+      __syncthreads();
+      // Offset of row i of the chunk in a plane (page 0 stands in where there is no page), and its page.
+      auto row_at = [&](int i, int32_t* page) {
+        const uint32_t r = (uint32_t)(r0 + i), p = a.pages.rows.div(r);
+        *page = sh.page[p - p0];
+        return max(*page, 0) * a.pages.page_stride + (int64_t)(r - p * page_rows) * a.pages.row_stride;
+      };
+
+      for (int i0 = wave * kStep; i0 < rows; i0 += kWaves * kStep) {
+        S st;
+        int32_t page, pages_of[kKeys];
 #pragma unroll
-    for (int i = 0; i < kKeys; ++i)
-      st.v[i] = *reinterpret_cast<const typename S::VRow*>(
-          row_at(vb, min(i0 + 16 * (i / 4) + 4 * g + i % 4, rows - 1)) + n * S::kV);
-    f32x4 xt[kR];
-    st.logits(q, xt);
-    float x[kKeys];
+        for (int t = 0; t < kR; ++t) {
+          const T* src = kb + row_at(min(i0 + 16 * t + n, rows - 1), &page);
 #pragma unroll
-    for (int i = 0; i < kKeys; ++i) x[i] = xt[i / 4][i % 4];
-    if (holes || i0 + kStep > rows) {
-      // Rows left out: their logit is -inf whatever they hold, their V is 0.
-#pragma unroll
-      for (int i = 0; i < kKeys; ++i) {
-        const int r = i0 + 16 * (i / 4) + 4 * g + i % 4;
-        bool in = r < rows;
-        if (in && holes) {
-          in = page_of[a.pages.rows.div((uint32_t)(r0 + r)) - p0] >= 0;
-          if (in && a.mask) in = a.mask[seq * a.mask_stride + r0 + r] != 0;
+          for (int j = 0; j < S::kQ; ++j) st.k[t][j] = stream(reinterpret_cast<const u32x4*>(src + S::k_off(g, j)));
         }
-        if (!in) {
-          x[i] = -INFINITY;
-          st.v[i] = typename S::VRow{};
+        int32_t least = 0;
+#pragma unroll
+        for (int i = 0; i < kKeys; ++i) {
+          const T* src = vb + row_at(min(i0 + 16 * (i / 4) + 4 * g + i % 4, rows - 1), &pages_of[i]) + n * S::kV;
+          st.v[i] = stream(reinterpret_cast<const typename S::VRow*>(src));
+          least = min(least, pages_of[i]);
         }
+        f32x4 xt[kR];
+        st.logits(q, xt);
+        float x[kKeys];
+#pragma unroll
+        for (int i = 0; i < kKeys; ++i) x[i] = xt[i / 4][i % 4];
+        if (a.mask || i0 + kStep > rows || __any(least < 0)) {
+          // Rows left out: their logit is -inf whatever they hold, their V is 0.
+#pragma unroll
+          for (int i = 0; i < kKeys; ++i) {
+            const int r = i0 + 16 * (i / 4) + 4 * g + i % 4;
+            bool in = r < rows && pages_of[i] >= 0;
+            if (in && a.mask) in = a.mask[seq * a.mask_stride + r0 + r] != 0;
+            if (!in) {
+              x[i] = -INFINITY;
+              st.v[i] = typename S::VRow{};
+            }
+          }
+        }
+        float top = x[0];
+#pragma unroll
+        for (int i = 1; i < kKeys; ++i) top = fmaxf(top, x[i]);
+        top = fmaxf(m, max_of_head(top));
+        const float at = top == -INFINITY ? 0.0f : top;   // no row yet: every exponent below is -inf
+        const float alpha = exp2_((m - at) * c);
+        m = top;
+        float sum = 0, p[kKeys];
+#pragma unroll
+        for (int i = 0; i < kKeys; ++i) {
+          p[i] = exp2_((x[i] - at) * c);
+          sum += p[i];
+        }
+        l = l * alpha + sum;
+#pragma unroll
+        for (int s = 0; s < S::kV; ++s) acc[s] *= alpha;
+        st.add(p, acc);
       }
     }
-    float top = x[0];
-#pragma unroll
-    for (int i = 1; i < kKeys; ++i) top = fmaxf(top, x[i]);
-    top = fmaxf(m, max_of_head(top));
-    const float at = top == -INFINITY ? 0.0f : top;   // no row yet: every exponent below is -inf
-    const float alpha = exp2_((m - at) * c);
-    m = top;
-    float sum = 0, p[kKeys];
-#pragma unroll
-    for (int i = 0; i < kKeys; ++i) {
-      p[i] = exp2_((x[i] - at) * c);
-      sum += p[i];
-    }
-    l = l * alpha + sum;
-#pragma unroll
-    for (int s = 0; s < S::kV; ++s) acc[s] *= alpha;
-    st.add(p, acc);
-  }
-  l = sum_of_head(l);
+    l = sum_of_head(l);
 
-  // Join the waves.  acc[s][i] is element (4 g + i) kV + s of head n.
-  if (g == 0) {
-    stat[wave][n][0] = m;
-    stat[wave][n][1] = l;
-  }
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int s = 0; s < S::kV; ++s) part[wave][n][(4 * g + i) * S::kV + s] = acc[s][i];
-  __syncthreads();
-  for (int i = threadIdx.x; i < heads * D; i += kThreads) {
-    const int h = i / D, e = i % D;
-    float top = -INFINITY;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, stat[w][h][0]);
-    const float at = top == -INFINITY ? 0.0f : top;
-    float sum = 0, o = 0;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      const float f = exp2_((stat[w][h][0] - at) * c);
-      sum += stat[w][h][1] * f;
-      o += part[w][h][e] * f;
+    // Join the waves.
+    if (g == 0) {
+      sh.stat[wave][n][0] = m;
+      sh.stat[wave][n][1] = l;
     }
-    const int64_t head = (int64_t)kh * a.group + h0 + h;
-    if (a.chunks > 1) {
-      float* to = a.part + ((seq * a.hkv * a.group + head) * a.chunks + chunk) * (D + 2);
-      to[e] = o;
-      if (e == 0) {
-        to[D] = top;
-        to[D + 1] = sum;
-      }
-    } else {
-      Elem<T>::put(sum > 0 ? o / sum : 0.0f, static_cast<T*>(a.out) + head * a.out_head + seq * a.out_row + e);
-      if (e == 0 && a.lse) a.lse[head * a.n_seq + seq] = sum > 0 ? top * a.scale + __log2f(sum) * kLn2 : -INFINITY;
-    }
-  }
-}
-
-// Joins the chunks of one head of one sequence.
-template <class T, int D>
-__global__ __launch_bounds__(kThreads) void k_join_chunks(const AttnArgs a) {
-  constexpr int kLanes = kThreads / D;
-  __shared__ float red[kThreads];
-  __shared__ float sums[kThreads];
-  const int64_t head = blockIdx.x, seq = blockIdx.y;
-  const int64_t width = (int64_t)a.pages.table_width * a.pages.rows.d;
-  const int64_t len = max((int64_t)0, min((int64_t)a.lens[seq], min(a.max_len, width)));
-  const int64_t lo = a.window > 0 ? max((int64_t)0, (int64_t)a.lens[seq] - a.window) : 0;
-  const int n = (int)((max((int64_t)0, len - lo) + a.chunk - 1) / a.chunk);
-  const float* part = a.part + (seq * a.hkv * a.group + head) * a.chunks * (D + 2);
-  const float c = a.scale * kLog2e;
-  float top = -INFINITY;
-  for (int i = threadIdx.x; i < n; i += kThreads) top = fmaxf(top, part[(int64_t)i * (D + 2) + D]);
-  red[threadIdx.x] = top;
-  __syncthreads();
-  for (int s = kThreads / 2; s > 0; s >>= 1) {
-    if (threadIdx.x < s) red[threadIdx.x] = fmaxf(red[threadIdx.x], red[threadIdx.x + s]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int s = 0; s < S::kV; s += 4)
+        *reinterpret_cast<f32x4*>(&sh.part[wave][n][(4 * g + i) * S::kV + s]) =
+            f32x4{acc[s][i], acc[s + 1][i], acc[s + 2][i], acc[s + 3][i]};
     __syncthreads();
-  }
-  top = red[0];
-  __syncthreads();
-  const float at = top == -INFINITY ? 0.0f : top;
-  const int e = threadIdx.x % D;
-  float o = 0, sum = 0;
-  for (int i = threadIdx.x / D; i < n; i += kLanes) {
-    const float* p = part + (int64_t)i * (D + 2);
-    const float f = exp2_((p[D] - at) * c);
-    o += p[e] * f;
-    sum += p[D + 1] * f;
-  }
-  red[threadIdx.x] = o;
-  sums[threadIdx.x] = sum;
-  __syncthreads();
-  if (threadIdx.x < D) {
-    o = sum = 0;
+    for (int i = threadIdx.x; i < heads * D; i += kThreads) {
+      const int h = i / D, e = i % D;
+      float top = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < kLanes; ++i) {
-      o += red[i * D + e];
-      sum += sums[i * D + e];
+      for (int w = 0; w < kWaves; ++w) top = fmaxf(top, sh.stat[w][h][0]);
+      const float at = top == -INFINITY ? 0.0f : top;
+      float sum = 0, o = 0;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        const float f = exp2_((sh.stat[w][h][0] - at) * c);
+        sum += sh.stat[w][h][1] * f;
+        o += sh.part[w][h][e] * f;
+      }
+      if (part) {
+        float* to = part + h * kPart<D>;
+        to[e] = o;
+        if (e == 0) {
+          to[D] = top;
+          to[D + 1] = sum;
+        }
+      } else {
+        const int64_t head = (int64_t)kh * a.group + h0 + h;
+        Elem<T>::put(sum > 0 ? o / sum : 0.0f, static_cast<T*>(a.out) + head * a.out_head + seq * a.out_row + e);
+        if (e == 0 && a.lse) a.lse[head * a.n_seq + seq] = sum > 0 ? top * a.scale + __log2f(sum) * kLn2 : -INFINITY;
+      }
     }
-    Elem<T>::put(sum > 0 ? o / sum : 0.0f, static_cast<T*>(a.out) + head * a.out_head + seq * a.out_row + e);
-    if (e == 0 && a.lse) a.lse[head * a.n_seq + seq] = sum > 0 ? top * a.scale + __log2f(sum) * kLn2 : -INFINITY;
+    __syncthreads();   // before the next item's parts
+  }
+};
+
+// One workgroup for each sequence and item.
+template <class T, int D>
+__global__ __launch_bounds__(64 * kWholeWaves) void k_attend_whole(const AttnArgs a) {
+  using W = Worker<T, D, kWholeWaves>;
+  __shared__ typename W::Shared sh;
+  const Rows of = rows_of(a, blockIdx.y);
+  W::run(a, sh, blockIdx.y, of, blockIdx.x, 0, of.tiles, nullptr);
+}
+
+// Share w of the tiles: those from w * all / shares on.
+__device__ __forceinline__ int64_t share_start(int64_t w, int64_t all, int64_t shares) { return w * all / shares; }
+
+template <class T, int D>
+__global__ __launch_bounds__(64 * kShareWaves, 3) void k_attend_shares(const AttnArgs a) {
+  using W = Worker<T, D, kShareWaves>;
+  constexpr int kThreads = W::kThreads;
+  __shared__ typename W::Shared sh;
+  __shared__ int64_t sums[kShareWaves];
+  __shared__ int64_t where[2];       // the first tile's sequence; the first tile of that sequence
+  const int items = a.hkv * a.tiles;
+
+  // Tiles of all sequences, and the sequence of this share's first one: each
+  // thread adds up a run of sequences.
+  const int64_t per = (a.n_seq + kThreads - 1) / kThreads;
+  const int64_t s0 = min(a.n_seq, threadIdx.x * per), s1 = min(a.n_seq, s0 + per);
+  int64_t mine = 0;
+  for (int64_t s = s0; s < s1; ++s) mine += (int64_t)rows_of(a, s).tiles * items;
+  int64_t upto = mine;               // tiles up to and with this thread's sequences
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int64_t x = __shfl_up((long long)upto, d);
+    if ((threadIdx.x & 63) >= (unsigned)d) upto += x;
+  }
+  if ((threadIdx.x & 63) == 63) sums[threadIdx.x >> 6] = upto;
+  __syncthreads();
+  int64_t all = 0;
+#pragma unroll
+  for (int w = 0; w < kShareWaves; ++w) {
+    if (w < (int)(threadIdx.x >> 6)) upto += sums[w];
+    all += sums[w];
+  }
+  // No more shares than give each wave a tile; none is empty.
+  const int64_t shares = max((int64_t)1, min((int64_t)a.shares, all / kShareWaves));
+  if (blockIdx.x >= shares) return;
+  const int64_t x0 = share_start(blockIdx.x, all, shares), x1 = share_start(blockIdx.x + 1, all, shares);
+  int64_t at = upto - mine;
+  if (x0 >= at && x0 < at + mine) {
+    int64_t s = s0;
+    for (;; ++s) {
+      const int64_t n = (int64_t)rows_of(a, s).tiles * items;
+      if (x0 < at + n) break;
+      at += n;
+    }
+    where[0] = s;
+    where[1] = at;
+  }
+  __syncthreads();
+  int64_t seq = where[0], base = where[1];
+  Rows of = rows_of(a, seq);
+  for (int64_t x = x0; x < x1;) {
+    const int item = (int)((x - base) / of.tiles);
+    const int64_t first = base + (int64_t)item * of.tiles;   // the item's first tile
+    const int t0 = (int)(x - first), t1 = (int)min((int64_t)of.tiles, t0 + (x1 - x));
+    const bool whole = t0 == 0 && t1 == of.tiles;
+    const int slot = 2 * (int)blockIdx.x + (x == x0 ? 0 : 1);
+    if (threadIdx.x == 0 && t0 == 0) {
+      // The item's last share is the last w with w all < (its last tile + 1) shares.
+      const int64_t last = ((first + of.tiles) * shares - 1) / all;
+      int32_t* to = a.split + 3 * (seq * items + item);
+      to[0] = whole ? 0 : (int32_t)(last - blockIdx.x) + 1;
+      to[1] = slot;
+      to[2] = blockIdx.x;
+    }
+    float* part = whole ? nullptr : a.part + (int64_t)slot * min(kHeads, a.group) * kPart<D>;
+    W::run(a, sh, seq, of, item, t0, t1, part);
+    x += t1 - t0;
+    if (x < x1 && x == base + (int64_t)items * of.tiles) {
+      base = x;
+      of = rows_of(a, ++seq);
+    }
   }
 }
 
-// Rows of a chunk: whole steps of a workgroup, as many as leave 1024 workgroups.
-void plan(int64_t n_seq, int64_t items, int64_t span, int32_t* chunk, int32_t* chunks) {
-  const int64_t want = std::max<int64_t>(1, 1024 / std::max<int64_t>(1, n_seq * items));
-  int64_t c = (span + want - 1) / want;
-  c = (c + kMinChunk - 1) / kMinChunk * kMinChunk;
-  c = std::min<int64_t>(std::max<int64_t>(c, kMinChunk), kMaxChunk);
-  *chunk = (int32_t)c;
-  *chunks = (int32_t)std::max<int64_t>(1, (span + c - 1) / c);
+// Joins the parts of one head of one sequence: groups of D/4 lanes each run over
+// every kGroups-th part, in order, and the groups are joined in order.
+template <class T, int D, int kThreads>
+__global__ __launch_bounds__(kThreads) void k_join_parts(const AttnArgs a) {
+  constexpr int kGroups = kThreads / (D / 4);
+  __shared__ f32x4 out[kGroups][D / 4];
+  __shared__ float stat[kGroups][2];
+  const int head = blockIdx.x;
+  const int64_t seq = blockIdx.y;
+  const int kh = head / a.group, h = head % a.group;
+  const int32_t* sp = a.split + 3 * (seq * a.hkv * a.tiles + (int64_t)kh * a.tiles + h / kHeads);
+  const int n = sp[0], slot0 = sp[1], w0 = sp[2];
+  if (n == 0) return;   // its output is written
+  const int64_t step = (int64_t)min(kHeads, a.group) * kPart<D>;
+  const float* base = a.part + (h % kHeads) * kPart<D>;
+  const float c = a.scale * kLog2e;
+  const int e4 = threadIdx.x % (D / 4), group = threadIdx.x / (D / 4);
+  float m = -INFINITY, sum = 0;
+  f32x4 o = {0, 0, 0, 0};
+#pragma unroll 4
+  for (int i = group; i < n; i += kGroups) {
+    const float* p = base + (i == 0 ? slot0 : 2 * (w0 + i)) * step;
+    const f32x4 x = *reinterpret_cast<const f32x4*>(p + 4 * e4);
+    const float mi = p[D], si = p[D + 1];
+    const float top = fmaxf(m, mi), at = top == -INFINITY ? 0.0f : top;
+    const float f = exp2_((m - at) * c), fi = exp2_((mi - at) * c);
+    o = o * f + x * fi;
+    sum = sum * f + si * fi;
+    m = top;
+  }
+  out[group][e4] = o;
+  if (e4 == 0) {
+    stat[group][0] = m;
+    stat[group][1] = sum;
+  }
+  __syncthreads();
+  for (int e = threadIdx.x; e < D; e += kThreads) {
+    float top = -INFINITY, r = 0, s = 0;
+#pragma unroll
+    for (int i = 0; i < kGroups; ++i) top = fmaxf(top, stat[i][0]);
+    const float at = top == -INFINITY ? 0.0f : top;
+#pragma unroll
+    for (int i = 0; i < kGroups; ++i) {
+      const float f = exp2_((stat[i][0] - at) * c);
+      r += out[i][e / 4][e % 4] * f;
+      s += stat[i][1] * f;
+    }
+    Elem<T>::put(s > 0 ? r / s : 0.0f, static_cast<T*>(a.out) + head * a.out_head + seq * a.out_row + e);
+    if (e == 0 && a.lse) a.lse[head * a.n_seq + seq] = s > 0 ? top * a.scale + __log2f(s) * kLn2 : -INFINITY;
+  }
+}
+
+constexpr int64_t kWholeSpan = 512;
+
+// Workgroups of k_attend_shares, 0 for one workgroup per sequence and item.
+int64_t plan(int64_t n_seq, int64_t items, int64_t span) {
+  const int64_t tiles = std::max<int64_t>(1, (span + kTile - 1) / kTile);
+  if (span <= kWholeSpan) return 0;
+  return std::min<int64_t>(kShares, (n_seq * items * tiles + kShareWaves - 1) / kShareWaves);
 }
 
 bool sizes_ok(int64_t n_seq, int32_t hq, int32_t hkv, int32_t d, int64_t max_len) {
   return n_seq >= 0 && n_seq < 65536 && hkv >= 1 && hkv < 65536 && hq >= hkv && hq % hkv == 0 && hq < 65536 &&
-         (d == 64 || d == 128) && max_len >= 0 && max_len < (int64_t(1) << 31) - kMaxChunk;
+         (d == 64 || d == 128) && max_len >= 0 && max_len < (int64_t(1) << 31) - kChunk;
 }
 
-// Bytes for the chunks of any span up to max_len.
-size_t workspace(int64_t n_seq, int32_t hq, int32_t hkv, int32_t d, int64_t max_len) {
-  const int64_t items = n_seq * hkv * ((hq / hkv + kHeads - 1) / kHeads);
-  const int64_t want = std::max<int64_t>(1, 1024 / std::max<int64_t>(1, items));
-  const int64_t chunks = std::max(std::min(want, (max_len + kMinChunk - 1) / kMinChunk), (max_len + kMaxChunk - 1) / kMaxChunk);
-  return chunks > 1 ? align_up((size_t)n_seq * hq * chunks * (d + 2) * sizeof(float)) : 0;
+struct Layout {
+  int32_t* split;
+  float* part;
+  size_t bytes;
+};
+
+// `shares` workgroups' parts, and which items are split.
+Layout layout(void* ws, int64_t shares, int64_t n_seq, int64_t items, int32_t group, int32_t d) {
+  Carver c(ws);
+  Layout l{nullptr, nullptr, 0};
+  if (shares) {
+    l.split = c.take<int32_t>(3 * (size_t)(n_seq * items));
+    l.part = c.take<float>((size_t)2 * shares * std::min(kHeads, group) * (d + 4));
+  }
+  l.bytes = c.used;
+  return l;
 }
 
 template <class T, int D>
 apack_status run(const AttnArgs& a, int32_t hq, hipStream_t s) {
-  hipLaunchKernelGGL((k_paged_attention<T, D>), dim3((unsigned)a.chunks, (unsigned)(a.hkv * a.tiles), (unsigned)a.n_seq),
-                     dim3(kThreads), 0, s, a);
-  apack_status st = launch_status("k_paged_attention");
-  if (st != APACK_OK || a.chunks == 1) return st;
-  hipLaunchKernelGGL((k_join_chunks<T, D>), dim3((unsigned)hq, (unsigned)a.n_seq), dim3(kThreads), 0, s, a);
-  return launch_status("k_join_chunks");
+  const unsigned items = (unsigned)(a.hkv * a.tiles);
+  if (a.shares == 0) {
+    hipLaunchKernelGGL((k_attend_whole<T, D>), dim3(items, (unsigned)a.n_seq), dim3(64 * kWholeWaves), 0, s, a);
+    return launch_status("k_attend_whole");
+  }
+  hipLaunchKernelGGL((k_attend_shares<T, D>), dim3((unsigned)a.shares), dim3(64 * kShareWaves), 0, s, a);
+  apack_status st = launch_status("k_attend_shares");
+  if (st != APACK_OK) return st;
+  // Few parts each: one wave a head; many: eight.
+  if (a.shares <= 8 * items * a.n_seq)
+    hipLaunchKernelGGL((k_join_parts<T, D, 64>), dim3((unsigned)hq, (unsigned)a.n_seq), dim3(64), 0, s, a);
+  else
+    hipLaunchKernelGGL((k_join_parts<T, D, 512>), dim3((unsigned)hq, (unsigned)a.n_seq), dim3(512), 0, s, a);
+  return launch_status("k_join_parts");
 }
 
 }  // namespace
@@ -395,7 +521,9 @@ extern "C" {
 
 size_t apack_paged_attention_workspace(int64_t n_seq, int32_t hq, int32_t hkv, int32_t d, int64_t max_len) {
   if (!sizes_ok(n_seq, hq, hkv, d, max_len)) return 0;
-  return std::max<size_t>(kAlign, workspace(n_seq, hq, hkv, d, max_len));
+  const int group = hq / hkv;
+  const int64_t items = (int64_t)hkv * ((group + kHeads - 1) / kHeads);
+  return std::max<size_t>(kAlign, layout(nullptr, plan(n_seq, items, max_len), n_seq, items, group, d).bytes);
 }
 
 apack_status apack_paged_attention(int64_t n_seq, int32_t hq, const apack_heads* q, const apack_heads* out, float* lse,
@@ -440,8 +568,10 @@ apack_status apack_paged_attention(int64_t n_seq, int32_t hq, const apack_heads*
   a.group = hq / pages->hkv;
   a.tiles = (a.group + kHeads - 1) / kHeads;
   APACK_CHECK((int64_t)a.hkv * a.tiles < 65536, APACK_E_UNSUPPORTED, "too many heads");
-  plan(n_seq, (int64_t)a.hkv * a.tiles, span, &a.chunk, &a.chunks);
-  const size_t need = a.chunks > 1 ? workspace(n_seq, hq, pages->hkv, pages->d, max_len) : 0;
+  const int64_t items = (int64_t)a.hkv * a.tiles;
+  a.shares = (int32_t)plan(n_seq, items, span);
+  const Layout lay = layout(ws, a.shares, n_seq, items, a.group, pages->d);
+  const size_t need = lay.bytes;
   if (need) {
     APACK_CHECK(ws && (uintptr_t)ws % kAlign == 0, APACK_E_WORKSPACE, "workspace must be non-NULL and 256-byte aligned");
     APACK_CHECK(ws_bytes >= need, APACK_E_WORKSPACE, "workspace %zu < %zu needed", ws_bytes, need);
@@ -464,7 +594,8 @@ apack_status apack_paged_attention(int64_t n_seq, int32_t hq, const apack_heads*
   a.v = pages->v[0];
   a.lens = lens;
   a.mask = mask;
-  a.part = static_cast<float*>(ws);
+  a.split = lay.split;
+  a.part = lay.part;
   a.mask_stride = mask_stride;
   a.max_len = max_len;
   a.window = window;
