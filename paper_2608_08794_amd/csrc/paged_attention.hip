@@ -37,7 +37,7 @@ constexpr int kTile = 32;         // rows of a tile
 constexpr int kChunk = 2048;      // rows whose page ids lie in LDS at a time
 constexpr int kShareWaves = 4;    // waves of a workgroup that takes a share
 constexpr int kWholeWaves = 8;    // ... that takes a sequence's key head whole
-constexpr int kShares = 768;      // three workgroups a compute unit: what the registers let run at once
+constexpr int kShares = 512;      // two workgroups a compute unit: what the registers let run at once
 template <int D> constexpr int kPart = D + 4;   // floats of a head's part: output, maximum, sum, 16-byte aligned
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
@@ -62,21 +62,29 @@ struct AttnArgs {
   PoolDev pages;
 };
 
-// Rows [lo, lo + n) that a sequence attends to, and their tiles (one, of no
-// rows, when there are none, so that its output is written).
+// Rows [base + skip, base + n) are those that a sequence attends to, base a
+// multiple of 16; n rows lie in so many tiles (one, of no rows, when there are
+// none, so that the output is written).
 struct Rows {
-  int64_t lo;
-  int n, tiles;
+  int64_t base;
+  int skip, n, tiles;
 };
 __device__ __forceinline__ Rows rows_of(const AttnArgs& a, int64_t seq) {
   const int64_t have = a.lens[seq];
   const int64_t len = max((int64_t)0, min(have, min(a.max_len, (int64_t)a.pages.table_width * a.pages.rows.d)));
   const int64_t lo = a.window > 0 ? max((int64_t)0, have - a.window) : 0;
-  const int n = (int)max((int64_t)0, len - lo);
-  return {lo, n, max(1, (n + kTile - 1) / kTile)};
+  const int64_t base = lo & ~(int64_t)15;
+  const int n = len > lo ? (int)(len - base) : 0;
+  return {base, (int)(lo - base), n, max(1, (n + kTile - 1) / kTile)};
 }
 
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// A value that all lanes hold, as the scalar that the compiler cannot see it is.
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ int64_t uniform(int64_t x) {
+  return (int64_t)((uint64_t)(uint32_t)uniform((int)x) | (uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32);
+}
 
 // Over the four lanes that hold a head.
 __device__ __forceinline__ float max_of_head(float x) {
@@ -177,44 +185,165 @@ template <int D> struct Step<float, D> {
 
 // A workgroup's state: per lane, for its head l % 16, the running maximum, its
 // keys' part of the sum, and acc[s][i], element (4 (l/16) + i) kV + s of the output.
-template <class T, int D, int kWaves>
+//
+// kAligned: pages hold a multiple of 16 rows, so the 16 rows of a logit tile lie
+// in one page.  A tile's address is then the wave's (scalar) plus an offset that a
+// lane keeps, and page ids sit in one register, lane by lane.  Otherwise every lane
+// looks its rows up in a list of page ids in LDS.
+template <class T, int D, int kWaves, bool kAligned>
 struct Worker {
   using S = Step<T, D>;
   static constexpr int kR = Elem<T>::kRow16, kKeys = 4 * kR, kStep = 16 * kR, kThreads = 64 * kWaves;
+  static constexpr int kIdSteps = 64 / kR;         // steps whose page ids a wave holds
   struct Shared {
-    int32_t page[kChunk + 1];       // ids of the pages of a chunk's rows, -1 where there is none
+    int32_t page[kAligned ? 1 : kChunk + 1];       // ids of the pages of a chunk's rows, -1 where there is none
     float part[kWaves][kHeads][D + 4];
     float stat[kWaves][kHeads][2];
   };
 
-  // Tiles [t0, t1) of item `item` (key head and 16 query heads) of a sequence.
-  // Writes the output, or with part != nullptr its parts.
-  static __device__ __forceinline__ void run(const AttnArgs& a, Shared& sh, int64_t seq, const Rows& of, int item, int t0,
-                                             int t1, float* part) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int n = lane & 15, g = lane >> 4;
-    const int kh = item / a.tiles, h0 = (item % a.tiles) * kHeads;
-    const int heads = min(kHeads, a.group - h0);
-    const uint32_t page_rows = a.pages.rows.d;
+  const AttnArgs& a;
+  Shared& sh;
+  const int64_t seq;
+  const Rows of;
+  const int kh, h0;                                // key head; first query head of its group
+  const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
+  const float c = a.scale * kLog2e;
+  u32x4 q[S::kQ];
+  float m = -INFINITY, l = 0;
+  f32x4 acc[S::kV] = {};
+  const T *kb, *vb;
 
+  __device__ __forceinline__ Worker(const AttnArgs& args, Shared& shared, int64_t s, const Rows& rows, int item)
+      : a(args), sh(shared), seq(s), of(rows), kh(item / args.tiles), h0((item % args.tiles) * kHeads) {
     // The query rows; heads past the group read its last one and are never stored.
-    u32x4 q[S::kQ];
-    {
-      const int h = kh * a.group + h0 + min(n, heads - 1);
-      const T* src = static_cast<const T*>(a.q) + h * a.q_head + seq * a.q_row;
+    const int h = kh * a.group + min(h0 + n, a.group - 1);
+    const T* src = static_cast<const T*>(a.q) + h * a.q_head + seq * a.q_row;
 #pragma unroll
-      for (int j = 0; j < S::kQ; ++j) q[j] = *reinterpret_cast<const u32x4*>(src + S::k_off(g, j));
-    }
-    const T* kb = static_cast<const T*>(a.k) + kh * a.pages.head_stride;
-    const T* vb = static_cast<const T*>(a.v) + kh * a.pages.head_stride;
-    const float c = a.scale * kLog2e;
-    float m = -INFINITY, l = 0;
-    f32x4 acc[S::kV] = {};
+    for (int j = 0; j < S::kQ; ++j) q[j] = *reinterpret_cast<const u32x4*>(src + S::k_off(g, j));
+    kb = static_cast<const T*>(a.k) + kh * a.pages.head_stride;
+    vb = static_cast<const T*>(a.v) + kh * a.pages.head_stride;
+  }
 
-    const int end = min(of.n, t1 * kTile);
-    for (int first = t0 * kTile; first < end; first += kChunk) {
+  // Takes a loaded step of rows from r0 on; page_in(i): whether key i lies in a page.  `holes`: some may not.
+  template <class F>
+  __device__ __forceinline__ void take(S& st, int r0, bool holes, F page_in) {
+    f32x4 xt[kR];
+    st.logits(q, xt);
+    float x[kKeys];
+#pragma unroll
+    for (int i = 0; i < kKeys; ++i) x[i] = xt[i / 4][i % 4];
+    if (holes || a.mask || r0 < of.skip || r0 + kStep > of.n) {
+      // Rows left out: their logit is -inf whatever they hold, their V is 0.
+      bool in[kKeys];
+#pragma unroll
+      for (int i = 0; i < kKeys; ++i) {
+        const int r = r0 + 16 * (i / 4) + 4 * g + i % 4;
+        in[i] = (r >= of.skip) & (r < of.n) & (!holes || page_in(i));
+      }
+      if (a.mask) {
+        const uint8_t* row = a.mask + seq * a.mask_stride + of.base;
+        uint8_t seen[kKeys];
+#pragma unroll
+        for (int i = 0; i < kKeys; ++i) seen[i] = row[min(r0 + 16 * (i / 4) + 4 * g + i % 4, of.n - 1)];
+#pragma unroll
+        for (int i = 0; i < kKeys; ++i) in[i] &= seen[i] != 0;
+      }
+#pragma unroll
+      for (int i = 0; i < kKeys; ++i) {
+        x[i] = in[i] ? x[i] : -INFINITY;
+        const uint32_t keep = in[i] ? ~0u : 0u;
+#pragma unroll
+        for (int e = 0; e < (int)(sizeof(typename S::VRow) / 4); ++e) st.v[i][e] &= keep;
+      }
+    }
+    float top = x[0];
+#pragma unroll
+    for (int i = 1; i < kKeys; ++i) top = fmaxf(top, x[i]);
+    top = fmaxf(m, max_of_head(top));
+    const float at = top == -INFINITY ? 0.0f : top;   // no row yet: every exponent below is -inf
+    const float alpha = exp2_((m - at) * c);
+    m = top;
+    float sum = 0, p[kKeys];
+#pragma unroll
+    for (int i = 0; i < kKeys; ++i) {
+      p[i] = exp2_((x[i] - at) * c);
+      sum += p[i];
+    }
+    l = l * alpha + sum;
+#pragma unroll
+    for (int s = 0; s < S::kV; ++s) acc[s] *= alpha;
+    st.add(p, acc);
+  }
+
+  // Rows [first, end), the waves' steps in turn.  Each step is loaded while the
+  // one before it is taken; a load past the last step reads one place of the pool.
+  __device__ __forceinline__ void rows_aligned(int first, int end) {
+    const int steps = max(0, (end - first - wave * kStep + kWaves * kStep - 1) / (kWaves * kStep));
+    if (steps == 0) return;
+    const int last = (of.n - 1) & ~15;              // first row of the last 16 that hold one
+    const uint32_t page_rows = a.pages.rows.d;
+    // Byte offsets of a lane's K row and first V row within 16 rows, and of a row.
+    const uint32_t row = (uint32_t)a.pages.row_stride * sizeof(T);
+    const uint32_t k_lane = n * row + S::k_off(g, 0) * sizeof(T);
+    const uint32_t v_lane = 4 * g * row + n * S::kV * sizeof(T);
+    auto row_of = [&](int s, int t) { return min(first + (wave + kWaves * s) * kStep + 16 * t, last); };
+    int32_t ids;
+    auto fetch_ids = [&](int s) {
+      if (s >= steps) return;
+      const uint32_t p = a.pages.rows.div((uint32_t)(of.base + row_of(s + lane / kR, lane % kR)));
+      ids = a.pages.table[seq * a.pages.table_stride + p];
+      asm volatile("" : "+v"(ids));                 // arrives here, not where it is read
+    };
+    auto load = [&](S& st, bool (&bad)[kR], int s) {
+      const bool live = s < steps;
+      const uint32_t ko = live ? k_lane : 0, vo = live ? v_lane : 0, step = live ? row : 0;
+#pragma unroll
+      for (int t = 0; t < kR; ++t) {
+        const int32_t id = __builtin_amdgcn_readlane(ids, s % kIdSteps * kR + t);
+        bad[t] = (uint32_t)id >= (uint32_t)a.pages.n_pages;
+        const uint32_t r = (uint32_t)of.base + row_of(s, t);
+        const int64_t at = (bad[t] || !live ? 0 : id) * a.pages.page_stride * (int64_t)sizeof(T) +
+                           (int64_t)(r - a.pages.rows.div(r) * page_rows) * row;
+        const char *k = reinterpret_cast<const char*>(kb) + at, *v = reinterpret_cast<const char*>(vb) + at;
+#pragma unroll
+        for (int j = 0; j < S::kQ; ++j)
+          st.k[t][j] = stream(reinterpret_cast<const u32x4*>(k + ko + (S::k_off(0, j) - S::k_off(0, 0)) * sizeof(T)));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t off = vo + i * step;
+          st.v[4 * t + i] = stream(reinterpret_cast<const typename S::VRow*>(v + off));
+        }
+      }
+    };
+    auto step = [&](S& st, const bool (&bad)[kR], int s) {
+      bool holes = false;
+#pragma unroll
+      for (int t = 0; t < kR; ++t) holes |= bad[t];
+      take(st, first + (wave + kWaves * s) * kStep, holes, [&](int i) { return !bad[i / 4]; });
+    };
+    S x, y;
+    bool bx[kR], by[kR];
+    // Loads are issued before the step that they overlap is begun.
+    fetch_ids(0);
+    load(x, bx, 0);
+    int s = 0;
+    for (; s + 1 < steps; s += 2) {
+      load(y, by, s + 1);
+      __builtin_amdgcn_sched_barrier(0);
+      step(x, bx, s);
+      if ((s + 2) % kIdSteps == 0) fetch_ids(s + 2);
+      load(x, bx, s + 2);
+      __builtin_amdgcn_sched_barrier(0);
+      step(y, by, s + 1);
+    }
+    if (s < steps) step(x, bx, s);
+  }
+
+  __device__ __forceinline__ void rows_general(int first, int end) {
+    const uint32_t page_rows = a.pages.rows.d;
+    for (; first < end; first += kChunk) {
       const int rows = min(kChunk, end - first);
-      const int64_t r0 = of.lo + first;
+      const int64_t r0 = of.base + first;
       const uint32_t p0 = a.pages.rows.div((uint32_t)r0);
       const int pages = (int)(a.pages.rows.div((uint32_t)(r0 + rows - 1)) - p0) + 1;
       __syncthreads();   // the last chunk's ids have been read
@@ -225,67 +354,34 @@ struct Worker {
       __syncthreads();
       // Offset of row i of the chunk in a plane (page 0 stands in where there is no page), and its page.
       auto row_at = [&](int i, int32_t* page) {
-        const uint32_t r = (uint32_t)(r0 + i), p = a.pages.rows.div(r);
+        const uint32_t r = (uint32_t)(r0 + min(i, rows - 1)), p = a.pages.rows.div(r);
         *page = sh.page[p - p0];
         return max(*page, 0) * a.pages.page_stride + (int64_t)(r - p * page_rows) * a.pages.row_stride;
       };
-
       for (int i0 = wave * kStep; i0 < rows; i0 += kWaves * kStep) {
         S st;
-        int32_t page, pages_of[kKeys];
+        int32_t page, least = 0, in[kKeys];
 #pragma unroll
         for (int t = 0; t < kR; ++t) {
-          const T* src = kb + row_at(min(i0 + 16 * t + n, rows - 1), &page);
+          const T* src = kb + row_at(i0 + 16 * t + n, &page);
 #pragma unroll
           for (int j = 0; j < S::kQ; ++j) st.k[t][j] = stream(reinterpret_cast<const u32x4*>(src + S::k_off(g, j)));
         }
-        int32_t least = 0;
 #pragma unroll
         for (int i = 0; i < kKeys; ++i) {
-          const T* src = vb + row_at(min(i0 + 16 * (i / 4) + 4 * g + i % 4, rows - 1), &pages_of[i]) + n * S::kV;
+          const T* src = vb + row_at(i0 + 16 * (i / 4) + 4 * g + i % 4, &in[i]) + n * S::kV;
           st.v[i] = stream(reinterpret_cast<const typename S::VRow*>(src));
-          least = min(least, pages_of[i]);
+          least = min(least, in[i]);
         }
-        f32x4 xt[kR];
-        st.logits(q, xt);
-        float x[kKeys];
-#pragma unroll
-        for (int i = 0; i < kKeys; ++i) x[i] = xt[i / 4][i % 4];
-        if (a.mask || i0 + kStep > rows || __any(least < 0)) {
-          // Rows left out: their logit is -inf whatever they hold, their V is 0.
-#pragma unroll
-          for (int i = 0; i < kKeys; ++i) {
-            const int r = i0 + 16 * (i / 4) + 4 * g + i % 4;
-            bool in = r < rows && pages_of[i] >= 0;
-            if (in && a.mask) in = a.mask[seq * a.mask_stride + r0 + r] != 0;
-            if (!in) {
-              x[i] = -INFINITY;
-              st.v[i] = typename S::VRow{};
-            }
-          }
-        }
-        float top = x[0];
-#pragma unroll
-        for (int i = 1; i < kKeys; ++i) top = fmaxf(top, x[i]);
-        top = fmaxf(m, max_of_head(top));
-        const float at = top == -INFINITY ? 0.0f : top;   // no row yet: every exponent below is -inf
-        const float alpha = exp2_((m - at) * c);
-        m = top;
-        float sum = 0, p[kKeys];
-#pragma unroll
-        for (int i = 0; i < kKeys; ++i) {
-          p[i] = exp2_((x[i] - at) * c);
-          sum += p[i];
-        }
-        l = l * alpha + sum;
-#pragma unroll
-        for (int s = 0; s < S::kV; ++s) acc[s] *= alpha;
-        st.add(p, acc);
+        take(st, first + i0, __any(least < 0), [&](int i) { return in[i] >= 0; });
       }
     }
-    l = sum_of_head(l);
+  }
 
-    // Join the waves.
+  // Joins the waves and writes the output, or with part != nullptr its parts.
+  __device__ __forceinline__ void finish(float* part) {
+    const int heads = min(kHeads, a.group - h0);
+    l = sum_of_head(l);
     if (g == 0) {
       sh.stat[wave][n][0] = m;
       sh.stat[wave][n][1] = l;
@@ -325,76 +421,86 @@ struct Worker {
     }
     __syncthreads();   // before the next item's parts
   }
+
+  // Tiles [t0, t1) of item `item` (key head and 16 query heads) of a sequence.
+  static __device__ __forceinline__ void run(const AttnArgs& a, Shared& sh, int64_t seq, const Rows& of, int item, int t0,
+                                             int t1, float* part) {
+    Worker w(a, sh, seq, of, item);
+    const int end = min(of.n, t1 * kTile);
+    if constexpr (kAligned) w.rows_aligned(t0 * kTile, end);
+    else w.rows_general(t0 * kTile, end);
+    w.finish(part);
+  }
 };
 
 // One workgroup for each sequence and item.
-template <class T, int D>
+template <class T, int D, bool kAligned>
 __global__ __launch_bounds__(64 * kWholeWaves) void k_attend_whole(const AttnArgs a) {
-  using W = Worker<T, D, kWholeWaves>;
+  using W = Worker<T, D, kWholeWaves, kAligned>;
   __shared__ typename W::Shared sh;
   const Rows of = rows_of(a, blockIdx.y);
   W::run(a, sh, blockIdx.y, of, blockIdx.x, 0, of.tiles, nullptr);
 }
 
-// Share w of the tiles: those from w * all / shares on.
-__device__ __forceinline__ int64_t share_start(int64_t w, int64_t all, int64_t shares) { return w * all / shares; }
+// a / b for 0 <= a < 2^50 and b > 0: the fp64 quotient is off by less than one.
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
+  int64_t q = (int64_t)((double)a * (1.0 / (double)b));
+  const int64_t r = a - q * b;
+  return r < 0 ? q - 1 : r >= b ? q + 1 : q;
+}
 
-template <class T, int D>
-__global__ __launch_bounds__(64 * kShareWaves, 3) void k_attend_shares(const AttnArgs a) {
-  using W = Worker<T, D, kShareWaves>;
-  constexpr int kThreads = W::kThreads;
+// Sum of x over the lanes up to and with this one.
+__device__ __forceinline__ uint32_t sum_upto(uint32_t x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);   // row_shr:1, 2, 4, 8: within 16 lanes
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);   // row_bcast:15 into rows 1 and 3
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);   // row_bcast:31 into rows 2 and 3
+  return x;
+}
+
+// Share w of `all` tiles: those from w all / shares on, rounded down.
+__device__ __forceinline__ int64_t share_start(int64_t w, int64_t all, int64_t shares) {
+  return quotient(w * all, shares);
+}
+
+template <class T, int D, bool kAligned>
+__global__ __launch_bounds__(64 * kShareWaves, 2) void k_attend_shares(const AttnArgs a) {
+  using W = Worker<T, D, kShareWaves, kAligned>;
   __shared__ typename W::Shared sh;
-  __shared__ int64_t sums[kShareWaves];
-  __shared__ int64_t where[2];       // the first tile's sequence; the first tile of that sequence
   const int items = a.hkv * a.tiles;
 
   // Tiles of all sequences, and the sequence of this share's first one: each
-  // thread adds up a run of sequences.
-  const int64_t per = (a.n_seq + kThreads - 1) / kThreads;
-  const int64_t s0 = min(a.n_seq, threadIdx.x * per), s1 = min(a.n_seq, s0 + per);
-  int64_t mine = 0;
-  for (int64_t s = s0; s < s1; ++s) mine += (int64_t)rows_of(a, s).tiles * items;
-  int64_t upto = mine;               // tiles up to and with this thread's sequences
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int64_t x = __shfl_up((long long)upto, d);
-    if ((threadIdx.x & 63) >= (unsigned)d) upto += x;
-  }
-  if ((threadIdx.x & 63) == 63) sums[threadIdx.x >> 6] = upto;
-  __syncthreads();
-  int64_t all = 0;
-#pragma unroll
-  for (int w = 0; w < kShareWaves; ++w) {
-    if (w < (int)(threadIdx.x >> 6)) upto += sums[w];
-    all += sums[w];
-  }
+  // lane adds up a run of sequences, every wave for itself (no barrier).
+  const int lane = threadIdx.x & 63;
+  const int64_t per = (a.n_seq + 63) / 64;
+  uint32_t mine = 0;
+  for (int64_t i = 0; i < per; ++i)
+    if (lane * per + i < a.n_seq) mine += rows_of(a, lane * per + i).tiles;
+  const uint32_t upto = sum_upto(mine);
+  const int64_t all = (int64_t)(uint32_t)__builtin_amdgcn_readlane(upto, 63) * items;
   // No more shares than give each wave a tile; none is empty.
   const int64_t shares = max((int64_t)1, min((int64_t)a.shares, all / kShareWaves));
   if (blockIdx.x >= shares) return;
   const int64_t x0 = share_start(blockIdx.x, all, shares), x1 = share_start(blockIdx.x + 1, all, shares);
-  int64_t at = upto - mine;
-  if (x0 >= at && x0 < at + mine) {
-    int64_t s = s0;
-    for (;; ++s) {
-      const int64_t n = (int64_t)rows_of(a, s).tiles * items;
-      if (x0 < at + n) break;
-      at += n;
-    }
-    where[0] = s;
-    where[1] = at;
-  }
-  __syncthreads();
-  int64_t seq = where[0], base = where[1];
+  const int owner = __popcll(__ballot((int64_t)upto * items <= x0));   // the lane whose run holds tile x0
+  int64_t seq = owner * per;
+  int64_t base = (int64_t)(uint32_t)(__builtin_amdgcn_readlane(upto, owner) - __builtin_amdgcn_readlane(mine, owner)) * items;
   Rows of = rows_of(a, seq);
+  while (x0 >= base + (int64_t)of.tiles * items) {
+    base += (int64_t)of.tiles * items;
+    of = rows_of(a, ++seq);
+  }
   for (int64_t x = x0; x < x1;) {
-    const int item = (int)((x - base) / of.tiles);
+    const int item = (int)quotient(x - base, of.tiles);
     const int64_t first = base + (int64_t)item * of.tiles;   // the item's first tile
     const int t0 = (int)(x - first), t1 = (int)min((int64_t)of.tiles, t0 + (x1 - x));
     const bool whole = t0 == 0 && t1 == of.tiles;
     const int slot = 2 * (int)blockIdx.x + (x == x0 ? 0 : 1);
     if (threadIdx.x == 0 && t0 == 0) {
       // The item's last share is the last w with w all < (its last tile + 1) shares.
-      const int64_t last = ((first + of.tiles) * shares - 1) / all;
+      const int64_t last = whole ? 0 : quotient((first + of.tiles) * shares - 1, all);
       int32_t* to = a.split + 3 * (seq * items + item);
       to[0] = whole ? 0 : (int32_t)(last - blockIdx.x) + 1;
       to[1] = slot;
@@ -471,9 +577,11 @@ int64_t plan(int64_t n_seq, int64_t items, int64_t span) {
   return std::min<int64_t>(kShares, (n_seq * items * tiles + kShareWaves - 1) / kShareWaves);
 }
 
+// Tiles of all sequences are counted in 32 bits, and times key heads and shares stay below 2^50.
 bool sizes_ok(int64_t n_seq, int32_t hq, int32_t hkv, int32_t d, int64_t max_len) {
-  return n_seq >= 0 && n_seq < 65536 && hkv >= 1 && hkv < 65536 && hq >= hkv && hq % hkv == 0 && hq < 65536 &&
-         (d == 64 || d == 128) && max_len >= 0 && max_len < (int64_t(1) << 31) - kChunk;
+  return n_seq >= 0 && n_seq < 65536 && hkv >= 1 && hkv < 256 && hq >= hkv && hq % hkv == 0 && hq < 4096 &&
+         (d == 64 || d == 128) && max_len >= 0 && max_len < (int64_t(1) << 31) - kChunk &&
+         n_seq * (max_len / kTile + 1) < (int64_t(1) << 31);
 }
 
 struct Layout {
@@ -494,14 +602,14 @@ Layout layout(void* ws, int64_t shares, int64_t n_seq, int64_t items, int32_t gr
   return l;
 }
 
-template <class T, int D>
-apack_status run(const AttnArgs& a, int32_t hq, hipStream_t s) {
+template <class T, int D, bool kAligned>
+apack_status launch(const AttnArgs& a, int32_t hq, hipStream_t s) {
   const unsigned items = (unsigned)(a.hkv * a.tiles);
   if (a.shares == 0) {
-    hipLaunchKernelGGL((k_attend_whole<T, D>), dim3(items, (unsigned)a.n_seq), dim3(64 * kWholeWaves), 0, s, a);
+    hipLaunchKernelGGL((k_attend_whole<T, D, kAligned>), dim3(items, (unsigned)a.n_seq), dim3(64 * kWholeWaves), 0, s, a);
     return launch_status("k_attend_whole");
   }
-  hipLaunchKernelGGL((k_attend_shares<T, D>), dim3((unsigned)a.shares), dim3(64 * kShareWaves), 0, s, a);
+  hipLaunchKernelGGL((k_attend_shares<T, D, kAligned>), dim3((unsigned)a.shares), dim3(64 * kShareWaves), 0, s, a);
   apack_status st = launch_status("k_attend_shares");
   if (st != APACK_OK) return st;
   // Few parts each: one wave a head; many: eight.
@@ -510,6 +618,13 @@ apack_status run(const AttnArgs& a, int32_t hq, hipStream_t s) {
   else
     hipLaunchKernelGGL((k_join_parts<T, D, 512>), dim3((unsigned)hq, (unsigned)a.n_seq), dim3(512), 0, s, a);
   return launch_status("k_join_parts");
+}
+
+template <class T, int D>
+apack_status run(const AttnArgs& a, int32_t hq, hipStream_t s) {
+  // 16 rows in one page, and offsets within them that 32 bits hold.
+  const bool aligned = a.pages.rows.d % 16 == 0 && a.pages.row_stride < (int64_t(1) << 26);
+  return aligned ? launch<T, D, true>(a, hq, s) : launch<T, D, false>(a, hq, s);
 }
 
 }  // namespace
@@ -567,7 +682,6 @@ apack_status apack_paged_attention(int64_t n_seq, int32_t hq, const apack_heads*
   a.hkv = pages->hkv;
   a.group = hq / pages->hkv;
   a.tiles = (a.group + kHeads - 1) / kHeads;
-  APACK_CHECK((int64_t)a.hkv * a.tiles < 65536, APACK_E_UNSUPPORTED, "too many heads");
   const int64_t items = (int64_t)a.hkv * a.tiles;
   a.shares = (int32_t)plan(n_seq, items, span);
   const Layout lay = layout(ws, a.shares, n_seq, items, a.group, pages->d);
