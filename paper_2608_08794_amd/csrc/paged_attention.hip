@@ -34,10 +34,9 @@ typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kHeads = 16;        // query heads of a workgroup: an MFMA's columns
 constexpr int kTile = 32;         // rows of a tile
-constexpr int kChunk = 2048;      // rows whose page ids lie in LDS at a time
-constexpr int kShareWaves = 4;    // waves of a workgroup that takes a share
-constexpr int kWholeWaves = 8;    // ... that takes a sequence's key head whole
-constexpr int kShares = 512;      // two workgroups a compute unit: what the registers let run at once
+constexpr int kWaves = 4;         // of a workgroup
+constexpr int kLeast = 1;         // tiles of the smallest share: with 4, one for each wave, 1312 rows of 8 over 2 heads take 11.6 us, not 8.8
+constexpr int kShares = 2048 / kWaves;   // eight waves a compute unit: what the registers let run at once
 template <int D> constexpr int kPart = D + 4;   // floats of a head's part: output, maximum, sum, 16-byte aligned
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
@@ -127,6 +126,7 @@ template <int D> struct Step<uint16_t, D> {
   using VRow = std::conditional_t<D == 128, u32x4, u32x2>;
   u32x4 k[2][kQ];
   VRow v[8];
+  uint32_t seen[2];     // mask bytes of the lane's keys
 
   static __device__ __forceinline__ int k_off(int g, int j) { return j * 32 + g * 8; }
 
@@ -142,16 +142,22 @@ template <int D> struct Step<uint16_t, D> {
   }
 
   __device__ __forceinline__ void add(const float (&p)[8], f32x4 (&acc)[kV]) const {
-    bf16x8 pb;
+    // Two bf16 parts hold 16 bits of each probability: their rounding stays below
+    // that of the result, and the second product costs nothing beside the loads.
+    bf16x8 hi, lo;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) pb[i] = (__bf16)p[i];
+    for (int i = 0; i < 8; ++i) {
+      hi[i] = (__bf16)p[i];
+      lo[i] = (__bf16)(p[i] - (float)hi[i]);
+    }
 #pragma unroll
     for (int s = 0; s < kV; ++s) {
       u32x4 a;
 #pragma unroll
       for (int j = 0; j < 4; ++j)   // element s of keys 2j and 2j + 1
         a[j] = __builtin_amdgcn_perm(v[2 * j + 1][s / 2], v[2 * j][s / 2], s % 2 ? 0x07060302u : 0x05040100u);
-      acc[s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), pb, acc[s], 0, 0, 0);
+      acc[s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), hi, acc[s], 0, 0, 0);
+      acc[s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), lo, acc[s], 0, 0, 0);
     }
   }
 };
@@ -162,6 +168,7 @@ template <int D> struct Step<float, D> {
   typedef unsigned int VRow __attribute__((ext_vector_type(kV)));
   u32x4 k[1][kQ];
   VRow v[4];
+  uint32_t seen[1];
 
   static __device__ __forceinline__ int k_off(int g, int j) { return j * 16 + g * 4; }
 
@@ -183,45 +190,51 @@ template <int D> struct Step<float, D> {
   }
 };
 
-// A workgroup's state: per lane, for its head l % 16, the running maximum, its
-// keys' part of the sum, and acc[s][i], element (4 (l/16) + i) kV + s of the output.
+// A wave's state over one item (key head and up to 16 of its query heads) of a
+// sequence: per lane, for its head l % 16, the running maximum, its keys' part of
+// the sum, and acc[s][i], element (4 (l/16) + i) kV + s of the output.
 //
 // kAligned: pages hold a multiple of 16 rows, so the 16 rows of a logit tile lie
 // in one page.  A tile's address is then the wave's (scalar) plus an offset that a
 // lane keeps, and page ids sit in one register, lane by lane.  Otherwise every lane
-// looks its rows up in a list of page ids in LDS.
-template <class T, int D, int kWaves, bool kAligned>
-struct Worker {
+// looks its rows' pages up.  kMask: there is a mask.
+template <class T, int D, bool kAligned, bool kMask>
+struct Wave {
   using S = Step<T, D>;
-  static constexpr int kR = Elem<T>::kRow16, kKeys = 4 * kR, kStep = 16 * kR, kThreads = 64 * kWaves;
+  static constexpr int kR = Elem<T>::kRow16, kKeys = 4 * kR, kStep = 16 * kR;
   static constexpr int kIdSteps = 64 / kR;         // steps whose page ids a wave holds
-  struct Shared {
-    int32_t page[kAligned ? 1 : kChunk + 1];       // ids of the pages of a chunk's rows, -1 where there is none
-    float part[kWaves][kHeads][D + 4];
-    float stat[kWaves][kHeads][2];
-  };
 
   const AttnArgs& a;
-  Shared& sh;
   const int64_t seq;
   const Rows of;
-  const int kh, h0;                                // key head; first query head of its group
-  const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
+  const int kh, h0, heads;                         // key head; first query head of its group, and how many
+  const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
   const float c = a.scale * kLog2e;
   u32x4 q[S::kQ];
   float m = -INFINITY, l = 0;
   f32x4 acc[S::kV] = {};
   const T *kb, *vb;
 
-  __device__ __forceinline__ Worker(const AttnArgs& args, Shared& shared, int64_t s, const Rows& rows, int item)
-      : a(args), sh(shared), seq(s), of(rows), kh(item / args.tiles), h0((item % args.tiles) * kHeads) {
+  __device__ __forceinline__ Wave(const AttnArgs& args, int64_t s, const Rows& rows, int item)
+      : a(args), seq(s), of(rows), kh(item / args.tiles), h0((item % args.tiles) * kHeads),
+        heads(min(kHeads, args.group - h0)) {
     // The query rows; heads past the group read its last one and are never stored.
-    const int h = kh * a.group + min(h0 + n, a.group - 1);
+    const int h = kh * a.group + h0 + min(n, heads - 1);
     const T* src = static_cast<const T*>(a.q) + h * a.q_head + seq * a.q_row;
 #pragma unroll
     for (int j = 0; j < S::kQ; ++j) q[j] = *reinterpret_cast<const u32x4*>(src + S::k_off(g, j));
     kb = static_cast<const T*>(a.k) + kh * a.pages.head_stride;
     vb = static_cast<const T*>(a.v) + kh * a.pages.head_stride;
+  }
+
+  // The mask from the sequence's first row on, and whether a step from r0 on lies inside it: its
+  // bytes are then loaded with the step's rows, four at a time.
+  __device__ __forceinline__ const uint8_t* mask_row() const { return a.mask + seq * a.mask_stride + of.base; }
+  __device__ __forceinline__ bool mask_whole(int r0) const { return of.base + r0 + kStep <= a.max_len; }
+  __device__ __forceinline__ void load_mask(S& st, int r0) const {
+    if (!kMask || !mask_whole(r0)) return;
+#pragma unroll
+    for (int t = 0; t < kR; ++t) __builtin_memcpy(&st.seen[t], mask_row() + r0 + 16 * t + 4 * g, 4);
   }
 
   // Takes a loaded step of rows from r0 on; page_in(i): whether key i lies in a page.  `holes`: some may not.
@@ -232,7 +245,7 @@ struct Worker {
     float x[kKeys];
 #pragma unroll
     for (int i = 0; i < kKeys; ++i) x[i] = xt[i / 4][i % 4];
-    if (holes || a.mask || r0 < of.skip || r0 + kStep > of.n) {
+    if (kMask || holes || r0 < of.skip || r0 + kStep > of.n) {
       // Rows left out: their logit is -inf whatever they hold, their V is 0.
       bool in[kKeys];
 #pragma unroll
@@ -240,11 +253,15 @@ struct Worker {
         const int r = r0 + 16 * (i / 4) + 4 * g + i % 4;
         in[i] = (r >= of.skip) & (r < of.n) & (!holes || page_in(i));
       }
-      if (a.mask) {
-        const uint8_t* row = a.mask + seq * a.mask_stride + of.base;
+      if constexpr (kMask) {
         uint8_t seen[kKeys];
+        if (mask_whole(r0)) {
 #pragma unroll
-        for (int i = 0; i < kKeys; ++i) seen[i] = row[min(r0 + 16 * (i / 4) + 4 * g + i % 4, of.n - 1)];
+          for (int i = 0; i < kKeys; ++i) seen[i] = (uint8_t)(st.seen[i / 4] >> 8 * (i % 4));
+        } else {
+#pragma unroll
+          for (int i = 0; i < kKeys; ++i) seen[i] = mask_row()[min(r0 + 16 * (i / 4) + 4 * g + i % 4, of.n - 1)];
+        }
 #pragma unroll
         for (int i = 0; i < kKeys; ++i) in[i] &= seen[i] != 0;
       }
@@ -275,18 +292,18 @@ struct Worker {
     st.add(p, acc);
   }
 
-  // Rows [first, end), the waves' steps in turn.  Each step is loaded while the
+  // Steps of rows first, first + stride, ... before `end`.  Each is loaded while the
   // one before it is taken; a load past the last step reads one place of the pool.
-  __device__ __forceinline__ void rows_aligned(int first, int end) {
-    const int steps = max(0, (end - first - wave * kStep + kWaves * kStep - 1) / (kWaves * kStep));
-    if (steps == 0) return;
+  __device__ __forceinline__ void rows_aligned(int first, int end, int stride) {
+    if (first >= end) return;
+    const int steps = (end - first + stride - 1) / stride;
     const int last = (of.n - 1) & ~15;              // first row of the last 16 that hold one
     const uint32_t page_rows = a.pages.rows.d;
     // Byte offsets of a lane's K row and first V row within 16 rows, and of a row.
     const uint32_t row = (uint32_t)a.pages.row_stride * sizeof(T);
     const uint32_t k_lane = n * row + S::k_off(g, 0) * sizeof(T);
     const uint32_t v_lane = 4 * g * row + n * S::kV * sizeof(T);
-    auto row_of = [&](int s, int t) { return min(first + (wave + kWaves * s) * kStep + 16 * t, last); };
+    auto row_of = [&](int s, int t) { return min(first + s * stride + 16 * t, last); };
     int32_t ids;
     auto fetch_ids = [&](int s) {
       if (s >= steps) return;
@@ -314,12 +331,13 @@ struct Worker {
           st.v[4 * t + i] = stream(reinterpret_cast<const typename S::VRow*>(v + off));
         }
       }
+      if (live) load_mask(st, first + s * stride);
     };
     auto step = [&](S& st, const bool (&bad)[kR], int s) {
       bool holes = false;
 #pragma unroll
       for (int t = 0; t < kR; ++t) holes |= bad[t];
-      take(st, first + (wave + kWaves * s) * kStep, holes, [&](int i) { return !bad[i / 4]; });
+      take(st, first + s * stride, holes, [&](int i) { return !bad[i / 4]; });
     };
     S x, y;
     bool bx[kR], by[kR];
@@ -339,107 +357,117 @@ struct Worker {
     if (s < steps) step(x, bx, s);
   }
 
-  __device__ __forceinline__ void rows_general(int first, int end) {
+  // The same for pages of any size; the next step's page ids are looked up while one is loaded.
+  __device__ __forceinline__ void rows_general(int first, int end, int stride) {
     const uint32_t page_rows = a.pages.rows.d;
-    for (; first < end; first += kChunk) {
-      const int rows = min(kChunk, end - first);
-      const int64_t r0 = of.base + first;
-      const uint32_t p0 = a.pages.rows.div((uint32_t)r0);
-      const int pages = (int)(a.pages.rows.div((uint32_t)(r0 + rows - 1)) - p0) + 1;
-      __syncthreads();   // the last chunk's ids have been read
-      for (int i = threadIdx.x; i < pages; i += kThreads) {
-        const int32_t p = a.pages.table[seq * a.pages.table_stride + p0 + i];
-        sh.page[i] = p >= 0 && p < a.pages.n_pages ? p : -1;
+    const int32_t* table = a.pages.table + seq * a.pages.table_stride;
+    // Row of the sequence that lane holds as K row t and as key i.
+    auto k_row = [&](int r0, int t) { return (uint32_t)(of.base + min(r0 + 16 * t + n, of.n - 1)); };
+    auto v_row = [&](int r0, int i) { return (uint32_t)(of.base + min(r0 + 16 * (i / 4) + 4 * g + i % 4, of.n - 1)); };
+    int32_t k_id[kR], v_id[kKeys];
+    auto fetch_ids = [&](int r0) {
+#pragma unroll
+      for (int t = 0; t < kR; ++t) k_id[t] = table[a.pages.rows.div(k_row(r0, t))];
+#pragma unroll
+      for (int i = 0; i < kKeys; ++i) v_id[i] = table[a.pages.rows.div(v_row(r0, i))];
+    };
+    // Offset of row r in a plane, of a page that may be none (page 0 stands in).
+    auto at = [&](uint32_t r, int32_t id) {
+      return ((uint32_t)id < (uint32_t)a.pages.n_pages ? id : 0) * a.pages.page_stride +
+             (int64_t)(r - a.pages.rows.div(r) * page_rows) * a.pages.row_stride;
+    };
+    if (first < end) fetch_ids(first);
+    for (int r0 = first; r0 < end; r0 += stride) {
+      S st;
+      bool bad[kKeys], any = false;
+#pragma unroll
+      for (int t = 0; t < kR; ++t) {
+        const T* src = kb + at(k_row(r0, t), k_id[t]);
+#pragma unroll
+        for (int j = 0; j < S::kQ; ++j) st.k[t][j] = stream(reinterpret_cast<const u32x4*>(src + S::k_off(g, j)));
       }
-      __syncthreads();
-      // Offset of row i of the chunk in a plane (page 0 stands in where there is no page), and its page.
-      auto row_at = [&](int i, int32_t* page) {
-        const uint32_t r = (uint32_t)(r0 + min(i, rows - 1)), p = a.pages.rows.div(r);
-        *page = sh.page[p - p0];
-        return max(*page, 0) * a.pages.page_stride + (int64_t)(r - p * page_rows) * a.pages.row_stride;
-      };
-      for (int i0 = wave * kStep; i0 < rows; i0 += kWaves * kStep) {
-        S st;
-        int32_t page, least = 0, in[kKeys];
 #pragma unroll
-        for (int t = 0; t < kR; ++t) {
-          const T* src = kb + row_at(i0 + 16 * t + n, &page);
-#pragma unroll
-          for (int j = 0; j < S::kQ; ++j) st.k[t][j] = stream(reinterpret_cast<const u32x4*>(src + S::k_off(g, j)));
-        }
-#pragma unroll
-        for (int i = 0; i < kKeys; ++i) {
-          const T* src = vb + row_at(i0 + 16 * (i / 4) + 4 * g + i % 4, &in[i]) + n * S::kV;
-          st.v[i] = stream(reinterpret_cast<const typename S::VRow*>(src));
-          least = min(least, in[i]);
-        }
-        take(st, first + i0, __any(least < 0), [&](int i) { return in[i] >= 0; });
+      for (int i = 0; i < kKeys; ++i) {
+        bad[i] = (uint32_t)v_id[i] >= (uint32_t)a.pages.n_pages;
+        any |= bad[i];
+        st.v[i] = stream(reinterpret_cast<const typename S::VRow*>(vb + at(v_row(r0, i), v_id[i]) + n * S::kV));
       }
+      load_mask(st, r0);
+      if (r0 + stride < end) fetch_ids(r0 + stride);
+      take(st, r0, __any(any), [&](int i) { return !bad[i]; });
     }
   }
 
-  // Joins the waves and writes the output, or with part != nullptr its parts.
-  __device__ __forceinline__ void finish(float* part) {
-    const int heads = min(kHeads, a.group - h0);
+  __device__ __forceinline__ void rows(int first, int end, int stride) {
+    if constexpr (kAligned) rows_aligned(first, end, stride);
+    else rows_general(first, end, stride);
     l = sum_of_head(l);
-    if (g == 0) {
-      sh.stat[wave][n][0] = m;
-      sh.stat[wave][n][1] = l;
+  }
+
+  __device__ __forceinline__ int64_t head(int h) const { return (int64_t)kh * a.group + h0 + h; }
+  __device__ __forceinline__ void put_lse(int h, float top, float sum) const {
+    if (a.lse) a.lse[head(h) * a.n_seq + seq] = sum > 0 ? top * a.scale + __log2f(sum) * kLn2 : -INFINITY;
+  }
+};
+
+// What the waves of a workgroup leave in LDS.
+template <int D>
+struct Joint {
+  float part[kWaves][kHeads][D + 4];
+  float stat[kWaves][kHeads][2];
+
+  // Joins the waves' states and writes the output, or its part.  Every thread calls it.
+  template <class W, class T>
+  __device__ __forceinline__ void join(const W& w, T* out, float* to_part) {
+    const int wave = threadIdx.x >> 6;
+    if (w.g == 0) {
+      stat[wave][w.n][0] = w.m;
+      stat[wave][w.n][1] = w.l;
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int s = 0; s < S::kV; s += 4)
-        *reinterpret_cast<f32x4*>(&sh.part[wave][n][(4 * g + i) * S::kV + s]) =
-            f32x4{acc[s][i], acc[s + 1][i], acc[s + 2][i], acc[s + 3][i]};
+      for (int s = 0; s < W::S::kV; s += 4)
+        *reinterpret_cast<f32x4*>(&part[wave][w.n][(4 * w.g + i) * W::S::kV + s]) =
+            f32x4{w.acc[s][i], w.acc[s + 1][i], w.acc[s + 2][i], w.acc[s + 3][i]};
     __syncthreads();
-    for (int i = threadIdx.x; i < heads * D; i += kThreads) {
+    for (int i = threadIdx.x; i < w.heads * D; i += 64 * kWaves) {
       const int h = i / D, e = i % D;
       float top = -INFINITY;
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) top = fmaxf(top, sh.stat[w][h][0]);
+      for (int v = 0; v < kWaves; ++v) top = fmaxf(top, stat[v][h][0]);
       const float at = top == -INFINITY ? 0.0f : top;
       float sum = 0, o = 0;
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) {
-        const float f = exp2_((sh.stat[w][h][0] - at) * c);
-        sum += sh.stat[w][h][1] * f;
-        o += sh.part[w][h][e] * f;
+      for (int v = 0; v < kWaves; ++v) {
+        const float f = exp2_((stat[v][h][0] - at) * w.c);
+        sum += stat[v][h][1] * f;
+        o += part[v][h][e] * f;
       }
-      if (part) {
-        float* to = part + h * kPart<D>;
+      if (to_part) {
+        float* to = to_part + h * kPart<D>;
         to[e] = o;
         if (e == 0) {
           to[D] = top;
           to[D + 1] = sum;
         }
       } else {
-        const int64_t head = (int64_t)kh * a.group + h0 + h;
-        Elem<T>::put(sum > 0 ? o / sum : 0.0f, static_cast<T*>(a.out) + head * a.out_head + seq * a.out_row + e);
-        if (e == 0 && a.lse) a.lse[head * a.n_seq + seq] = sum > 0 ? top * a.scale + __log2f(sum) * kLn2 : -INFINITY;
+        Elem<T>::put(sum > 0 ? o / sum : 0.0f, out + w.head(h) * w.a.out_head + w.seq * w.a.out_row + e);
+        if (e == 0) w.put_lse(h, top, sum);
       }
     }
-    __syncthreads();   // before the next item's parts
-  }
-
-  // Tiles [t0, t1) of item `item` (key head and 16 query heads) of a sequence.
-  static __device__ __forceinline__ void run(const AttnArgs& a, Shared& sh, int64_t seq, const Rows& of, int item, int t0,
-                                             int t1, float* part) {
-    Worker w(a, sh, seq, of, item);
-    const int end = min(of.n, t1 * kTile);
-    if constexpr (kAligned) w.rows_aligned(t0 * kTile, end);
-    else w.rows_general(t0 * kTile, end);
-    w.finish(part);
   }
 };
 
-// One workgroup for each sequence and item.
-template <class T, int D, bool kAligned>
-__global__ __launch_bounds__(64 * kWholeWaves) void k_attend_whole(const AttnArgs a) {
-  using W = Worker<T, D, kWholeWaves, kAligned>;
-  __shared__ typename W::Shared sh;
+// One workgroup for each sequence and item: its waves take the steps in turn.
+template <class T, int D, bool kAligned, bool kMask>
+__global__ __launch_bounds__(64 * kWaves, 2) void k_attend_whole(const AttnArgs a) {
+  using W = Wave<T, D, kAligned, kMask>;
+  __shared__ Joint<D> sh;
   const Rows of = rows_of(a, blockIdx.y);
-  W::run(a, sh, blockIdx.y, of, blockIdx.x, 0, of.tiles, nullptr);
+  W w(a, blockIdx.y, of, blockIdx.x);
+  w.rows(uniform((int)threadIdx.x >> 6) * W::kStep, of.n, kWaves * W::kStep);
+  sh.join(w, static_cast<T*>(a.out), nullptr);
 }
 
 // a / b for 0 <= a < 2^50 and b > 0: the fp64 quotient is off by less than one.
@@ -465,14 +493,14 @@ __device__ __forceinline__ int64_t share_start(int64_t w, int64_t all, int64_t s
   return quotient(w * all, shares);
 }
 
-template <class T, int D, bool kAligned>
-__global__ __launch_bounds__(64 * kShareWaves, 2) void k_attend_shares(const AttnArgs a) {
-  using W = Worker<T, D, kShareWaves, kAligned>;
-  __shared__ typename W::Shared sh;
+template <class T, int D, bool kAligned, bool kMask>
+__global__ __launch_bounds__(64 * kWaves, 2) void k_attend_shares(const AttnArgs a) {
   const int items = a.hkv * a.tiles;
+  const int share = blockIdx.x;
+  __shared__ Joint<D> sh;
 
   // Tiles of all sequences, and the sequence of this share's first one: each
-  // lane adds up a run of sequences, every wave for itself (no barrier).
+  // lane adds up a run of sequences.
   const int lane = threadIdx.x & 63;
   const int64_t per = (a.n_seq + 63) / 64;
   uint32_t mine = 0;
@@ -480,10 +508,10 @@ __global__ __launch_bounds__(64 * kShareWaves, 2) void k_attend_shares(const Att
     if (lane * per + i < a.n_seq) mine += rows_of(a, lane * per + i).tiles;
   const uint32_t upto = sum_upto(mine);
   const int64_t all = (int64_t)(uint32_t)__builtin_amdgcn_readlane(upto, 63) * items;
-  // No more shares than give each wave a tile; none is empty.
-  const int64_t shares = max((int64_t)1, min((int64_t)a.shares, all / kShareWaves));
-  if (blockIdx.x >= shares) return;
-  const int64_t x0 = share_start(blockIdx.x, all, shares), x1 = share_start(blockIdx.x + 1, all, shares);
+  // No share is smaller than kLeast tiles (as far as there are so many).
+  const int64_t shares = max((int64_t)1, min((int64_t)a.shares, all / kLeast));
+  if (share >= shares) return;
+  const int64_t x0 = share_start(share, all, shares), x1 = share_start(share + 1, all, shares);
   const int owner = __popcll(__ballot((int64_t)upto * items <= x0));   // the lane whose run holds tile x0
   int64_t seq = owner * per;
   int64_t base = (int64_t)(uint32_t)(__builtin_amdgcn_readlane(upto, owner) - __builtin_amdgcn_readlane(mine, owner)) * items;
@@ -497,17 +525,19 @@ __global__ __launch_bounds__(64 * kShareWaves, 2) void k_attend_shares(const Att
     const int64_t first = base + (int64_t)item * of.tiles;   // the item's first tile
     const int t0 = (int)(x - first), t1 = (int)min((int64_t)of.tiles, t0 + (x1 - x));
     const bool whole = t0 == 0 && t1 == of.tiles;
-    const int slot = 2 * (int)blockIdx.x + (x == x0 ? 0 : 1);
+    const int slot = 2 * share + (x == x0 ? 0 : 1);
+    Wave<T, D, kAligned, kMask> w(a, seq, of, item);
+    w.rows(t0 * kTile + uniform((int)threadIdx.x >> 6) * w.kStep, min(of.n, t1 * kTile), kWaves * w.kStep);
+    if (x > x0) __syncthreads();   // the item before has been read from LDS
+    sh.join(w, static_cast<T*>(a.out), whole ? nullptr : a.part + (int64_t)slot * min(kHeads, a.group) * kPart<D>);
     if (threadIdx.x == 0 && t0 == 0) {
-      // The item's last share is the last w with w all < (its last tile + 1) shares.
+      // The item's last share is the last one that starts before its end.
       const int64_t last = whole ? 0 : quotient((first + of.tiles) * shares - 1, all);
       int32_t* to = a.split + 3 * (seq * items + item);
-      to[0] = whole ? 0 : (int32_t)(last - blockIdx.x) + 1;
+      to[0] = whole ? 0 : (int32_t)(last - share) + 1;
       to[1] = slot;
-      to[2] = blockIdx.x;
+      to[2] = share;
     }
-    float* part = whole ? nullptr : a.part + (int64_t)slot * min(kHeads, a.group) * kPart<D>;
-    W::run(a, sh, seq, of, item, t0, t1, part);
     x += t1 - t0;
     if (x < x1 && x == base + (int64_t)items * of.tiles) {
       base = x;
@@ -570,17 +600,17 @@ __global__ __launch_bounds__(kThreads) void k_join_parts(const AttnArgs a) {
 
 constexpr int64_t kWholeSpan = 512;
 
-// Workgroups of k_attend_shares, 0 for one workgroup per sequence and item.
+// Shares of k_attend_shares, 0 for one workgroup per sequence and item.
 int64_t plan(int64_t n_seq, int64_t items, int64_t span) {
   const int64_t tiles = std::max<int64_t>(1, (span + kTile - 1) / kTile);
-  if (span <= kWholeSpan) return 0;
-  return std::min<int64_t>(kShares, (n_seq * items * tiles + kShareWaves - 1) / kShareWaves);
+  if (span <= kWholeSpan || (span <= 4 * kWholeSpan && n_seq * items >= 256)) return 0;
+  return std::min<int64_t>(kShares, (n_seq * items * tiles + kLeast - 1) / kLeast);
 }
 
 // Tiles of all sequences are counted in 32 bits, and times key heads and shares stay below 2^50.
 bool sizes_ok(int64_t n_seq, int32_t hq, int32_t hkv, int32_t d, int64_t max_len) {
   return n_seq >= 0 && n_seq < 65536 && hkv >= 1 && hkv < 256 && hq >= hkv && hq % hkv == 0 && hq < 4096 &&
-         (d == 64 || d == 128) && max_len >= 0 && max_len < (int64_t(1) << 31) - kChunk &&
+         (d == 64 || d == 128) && max_len >= 0 && max_len < (int64_t(1) << 31) - 64 &&
          n_seq * (max_len / kTile + 1) < (int64_t(1) << 31);
 }
 
@@ -602,14 +632,14 @@ Layout layout(void* ws, int64_t shares, int64_t n_seq, int64_t items, int32_t gr
   return l;
 }
 
-template <class T, int D, bool kAligned>
+template <class T, int D, bool kAligned, bool kMask>
 apack_status launch(const AttnArgs& a, int32_t hq, hipStream_t s) {
   const unsigned items = (unsigned)(a.hkv * a.tiles);
   if (a.shares == 0) {
-    hipLaunchKernelGGL((k_attend_whole<T, D, kAligned>), dim3(items, (unsigned)a.n_seq), dim3(64 * kWholeWaves), 0, s, a);
+    hipLaunchKernelGGL((k_attend_whole<T, D, kAligned, kMask>), dim3(items, (unsigned)a.n_seq), dim3(64 * kWaves), 0, s, a);
     return launch_status("k_attend_whole");
   }
-  hipLaunchKernelGGL((k_attend_shares<T, D, kAligned>), dim3((unsigned)a.shares), dim3(64 * kShareWaves), 0, s, a);
+  hipLaunchKernelGGL((k_attend_shares<T, D, kAligned, kMask>), dim3((unsigned)a.shares), dim3(64 * kWaves), 0, s, a);
   apack_status st = launch_status("k_attend_shares");
   if (st != APACK_OK) return st;
   // Few parts each: one wave a head; many: eight.
@@ -624,7 +654,8 @@ template <class T, int D>
 apack_status run(const AttnArgs& a, int32_t hq, hipStream_t s) {
   // 16 rows in one page, and offsets within them that 32 bits hold.
   const bool aligned = a.pages.rows.d % 16 == 0 && a.pages.row_stride < (int64_t(1) << 26);
-  return aligned ? launch<T, D, true>(a, hq, s) : launch<T, D, false>(a, hq, s);
+  if (a.mask) return aligned ? launch<T, D, true, true>(a, hq, s) : launch<T, D, false, true>(a, hq, s);
+  return aligned ? launch<T, D, true, false>(a, hq, s) : launch<T, D, false, false>(a, hq, s);
 }
 
 }  // namespace
