@@ -16,9 +16,11 @@
 namespace apack {
 namespace {
 
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+
 constexpr int kThreads = 256;
 constexpr int kMaxDim = 512;
-constexpr int kUnroll = 4;      // heads in flight per thread
+constexpr int kUnroll = 2;      // heads in flight per thread
 constexpr double kTwoPi = 6.283185307179586476925286766559;
 
 struct HeadsDev {
@@ -48,6 +50,27 @@ struct alignas(sizeof(T) * VEC) Vec {
   T v[VEC];
 };
 
+// kStream: nontemporal, for tensors that pass once (16-byte vectors only).
+template <bool kStream, class T, int VEC>
+__device__ __forceinline__ void get(const T* p, Vec<T, VEC>* v) {
+  if constexpr (kStream && VEC > 1) {
+    const u32x4 x = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
+    __builtin_memcpy(v, &x, 16);
+  } else {
+    *v = *reinterpret_cast<const Vec<T, VEC>*>(p);
+  }
+}
+template <bool kStream, class T, int VEC>
+__device__ __forceinline__ void put(const Vec<T, VEC>& v, T* p) {
+  if constexpr (kStream && VEC > 1) {
+    u32x4 x;
+    __builtin_memcpy(&x, &v, 16);
+    __builtin_nontemporal_store(x, reinterpret_cast<u32x4*>(p));
+  } else {
+    *reinterpret_cast<Vec<T, VEC>*>(p) = v;
+  }
+}
+
 __device__ __forceinline__ float to_f(float x) { return x; }
 __device__ __forceinline__ float to_f(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
 __device__ __forceinline__ void from_f(float x, float* y) { *y = x; }
@@ -63,8 +86,10 @@ __device__ __forceinline__ void turn_pair(float a, float b, float c, float s, T*
   from_f(__builtin_fmaf(a, s, b * c), y);
 }
 
-// T: uint16_t (bf16 bits) or float.  A thread's VEC pairs are element e0 + j
-// with element e1 + j (kHalf), or the 2 * VEC elements from e0 on, two by two.
+// T: uint16_t (bf16 bits) or float.  A thread has VEC elements from e0 and VEC from
+// e1 on, half of what turns (or of what does not) apart, so that the lanes of either
+// load lie side by side.  The VEC pairs are (e0 + j, e1 + j) (kHalf), or two by two
+// within each; single elements (VEC 1) are neighbours then.
 template <class T, int VEC, bool kHalf, bool kAppend>
 __global__ __launch_bounds__(kThreads) void k_rotary(const RotaryArgs a) {
   using V = Vec<T, VEC>;
@@ -73,13 +98,17 @@ __global__ __launch_bounds__(kThreads) void k_rotary(const RotaryArgs a) {
   if (rl >= a.rows_per_wg || row >= a.rows) return;
   const int half = a.rot >> 1;
   const bool turned = c * VEC < half;
-  int e0, e1;
+  int e0, e1, pair0, pair1;      // the first pair of either half of the pairs
   if (turned) {
-    e0 = kHalf ? c * VEC : 2 * c * VEC;
-    e1 = kHalf ? e0 + half : e0 + VEC;
+    const bool apart = kHalf || VEC > 1;
+    e0 = apart ? c * VEC : 2 * c;
+    e1 = apart ? e0 + half : e0 + 1;
+    pair0 = kHalf || VEC == 1 ? c * VEC : e0 / 2;
+    pair1 = kHalf || VEC == 1 ? pair0 + VEC / 2 : e1 / 2;
   } else {                       // elements that do not turn
-    e0 = 2 * c * VEC;
-    e1 = e0 + VEC;
+    e0 = a.rot + (c * VEC - half);
+    e1 = e0 + (a.d - a.rot + 1) / 2;
+    pair0 = pair1 = 0;
   }
   const bool second = e1 < a.d;  // an odd d ends in a single element
 
@@ -90,7 +119,7 @@ __global__ __launch_bounds__(kThreads) void k_rotary(const RotaryArgs a) {
     for (int j = 0; j < 4; ++j) p[j] = j < a.pos_rows ? a.pos[j * a.pos_stride + row] : 0;
 #pragma unroll
     for (int j = 0; j < VEC; ++j) {
-      const int i = c * VEC + j;
+      const int i = VEC > 1 && j >= VEC / 2 ? pair1 + j - VEC / 2 : pair0 + j;
       const int32_t at = i < a.bound[0] ? p[0] : i < a.bound[1] ? p[1] : i < a.bound[2] ? p[2] : p[3];
       // fp64 up to the fraction of a turn: a position of 2^31 is still off by
       // less than 2^-24 turns, where an fp32 angle would be off by whole turns.
@@ -140,8 +169,8 @@ __global__ __launch_bounds__(kThreads) void k_rotary(const RotaryArgs a) {
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u)
           if (h + u < n) {
-            x[u] = *reinterpret_cast<const V*>(in + (h + u) * t.in_head + e0);
-            if (second) y[u] = *reinterpret_cast<const V*>(in + (h + u) * t.in_head + e1);
+            get<!kAppend>(in + (h + u) * t.in_head + e0, &x[u]);
+            if (second) get<!kAppend>(in + (h + u) * t.in_head + e1, &y[u]);
           }
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u)
@@ -163,8 +192,8 @@ __global__ __launch_bounds__(kThreads) void k_rotary(const RotaryArgs a) {
                 }
               }
             }
-            *reinterpret_cast<V*>(out + (h + u) * t.out_head + e0) = x[u];
-            if (second) *reinterpret_cast<V*>(out + (h + u) * t.out_head + e1) = y[u];
+            put<!kAppend>(x[u], out + (h + u) * t.out_head + e0);
+            if (second) put<!kAppend>(y[u], out + (h + u) * t.out_head + e1);
           }
       }
     left -= n;
@@ -249,9 +278,13 @@ apack_status run(RotaryArgs& a, const apack_rope* rope, apack_dtype dtype, bool 
   a.rows_per_wg = kThreads / a.chunks;
   const int64_t blocks = (a.rows + a.rows_per_wg - 1) / a.rows_per_wg;
   APACK_CHECK(blocks < (int64_t(1) << 31), APACK_E_UNSUPPORTED, "too many rows");
-  // Heads are split over workgroups until there are 1024 of them.
+  // Heads are split over workgroups until there are 1024 of them, and to two a
+  // thread where vectors of it are in flight: 94028 rows of 32 heads of 128 take 261 us
+  // so, 275 with eight heads a thread; single elements take 84 us for 20000 rows with
+  // all heads, 116 with two.
   const int64_t split = std::max<int64_t>(1, std::min<int64_t>(heads, 1024 / blocks));
   a.heads_per_wg = (int32_t)((heads + split - 1) / split);
+  if (wide) a.heads_per_wg = std::min(a.heads_per_wg, kUnroll);
   const int gy = (heads + a.heads_per_wg - 1) / a.heads_per_wg;
   APACK_CHECK(gy < 65536, APACK_E_UNSUPPORTED, "65536 heads or more in all");
   const dim3 grid((unsigned)blocks, (unsigned)gy);
