@@ -57,14 +57,13 @@ def _fail(status, message):
     raise ApackError(status, message)
 
 
-def _on_device(*named):
-    """The device that every (tensor, name) lies on; it must be the current one."""
-    torch = _torch()
-    index = named[0][0].get_device()
-    for t, name in named:
+def _on_device(tensors, names):
+    """The device that every tensor lies on; it must be the current one.  names: theirs, in one text."""
+    index = tensors[0].get_device()
+    for i, t in enumerate(tensors):
         if t.get_device() != index or index < 0:
-            _fail(1, f"{name} must be a CUDA tensor on the call's device")
-    if index != torch.cuda.current_device():
+            _fail(1, f"{names.split()[i]} must be a CUDA tensor on the call's device")
+    if index != _torch().cuda.current_device():
         _fail(1, f"the tensors lie on device {index}, which is not the current one")
     return index
 
@@ -83,9 +82,10 @@ def _heads(t, name, dtype):
     if t.dim() != 3:
         _fail(2, f"{name} must be [heads, rows, d]")
     sh, sr, se = t.stride()
-    if se != 1 and t.shape[2] > 1:
+    heads, _, d = t.shape
+    if se != 1 and d > 1:
         _fail(2, f"{name} must have contiguous elements")
-    return Heads(t.data_ptr(), t.shape[0], 0, sh, sr)
+    return Heads(t.data_ptr(), heads, 0, sh, sr)
 
 
 def _int32(t, name, dims):
@@ -151,18 +151,43 @@ def _pages(k, v, table=None, n_seq=0, name="pages", planes=False):
         pages, (hkv, rows, d), (sh, sr, _), sp = 1, shape, stride, 0
     else:
         (pages, hkv, rows, d), (sp, sh, sr, _) = shape, stride
-    tp, width, ts = None, 0, 0
-    if table is not None:
-        if table.dtype is not _torch().int32:
-            _fail(3, f"the table must be int32, not {table.dtype}")
-        if table.dim() != 2 or table.shape[0] != n_seq:
-            _fail(2, f"the table must be [{n_seq}, pages]")
-        width = table.shape[1]
-        ts, se = table.stride()
-        if se != 1 and width > 1:
-            _fail(2, "the table must have contiguous rows")
-        tp, ts = table.data_ptr(), ts if n_seq > 1 else width
+    tp, width, ts = (None, 0, 0) if table is None else _table(table, n_seq)
     return Pages(n, pages, rows, hkv, d, width, _code(dtype), 0, sp, sh, sr, kp, vp, tp, ts)
+
+
+def _table(table, n_seq):
+    """(pointer, width, row stride) of a page table."""
+    if table.dtype is not _torch().int32:
+        _fail(3, f"the table must be int32, not {table.dtype}")
+    if table.dim() != 2 or table.shape[0] != n_seq:
+        _fail(2, f"the table must be [{n_seq}, pages]")
+    width = table.shape[1]
+    ts, se = table.stride()
+    if se != 1 and width > 1:
+        _fail(2, "the table must have contiguous rows")
+    return table.data_ptr(), width, ts if n_seq > 1 else width
+
+
+_P1 = _P * 1
+
+
+def _one_layer(k, v, dtype, table, n_seq, d):
+    """An apack_pages of one layer's [pages, heads, rows, d] K and V, as a decode step uses them."""
+    if k.dim() != 4:
+        _fail(2, "k_pages must be [pages, heads, rows, d]")
+    shape, stride = k.shape, k.stride()
+    if v.shape != shape or v.stride() != stride:
+        _fail(2, "v_pages must match k_pages in shape and strides")
+    if k.dtype is not dtype or v.dtype is not dtype:
+        _fail(3, "q and the pages must share a dtype")
+    pages, hkv, rows, width = shape
+    sp, sh, sr, se = stride
+    if width != d:
+        _fail(2, "q and the pages differ in d")
+    if se != 1 and d > 1:
+        _fail(2, "the pages must have contiguous elements")
+    tp, width, ts = _table(table, n_seq)
+    return Pages(1, pages, rows, hkv, d, width, _code(dtype), 0, sp, sh, sr, _P1(k.data_ptr()), _P1(v.data_ptr()), tp, ts)
 
 
 def _code(dtype):
@@ -174,8 +199,16 @@ def _code(dtype):
     _fail(3, f"unsupported dtype {dtype}")
 
 
+def _like(stream, x):
+    """A contiguous output of x's shape, allocated on the stream that the call runs on."""
+    torch = _torch()
+    if stream is None:
+        return torch.empty_like(x, memory_format=torch.contiguous_format)
+    with _alloc_on(stream):
+        return torch.empty_like(x, memory_format=torch.contiguous_format)
+
+
 def _new(stream, shape, dtype, device):
-    """An output, allocated on the stream that the call runs on."""
     torch = _torch()
     if stream is None:
         return torch.empty(shape, dtype=dtype, device=device)
@@ -244,8 +277,8 @@ def apack_rotary(pos, rope, q=None, k=None, q_out=None, k_out=None, transpose=No
         _fail(1, "an output without its input")
     if some.dim() != 3:
         _fail(2, "q and k must be [heads, rows, d]")
-    index = _on_device((pos, "pos"), *[(t, n) for t, n in ((q, "q"), (k, "k"), (q_out, "q_out"), (k_out, "k_out"))
-                                       if t is not None])
+    used = [(t, n) for t, n in ((pos, "pos"), (q, "q"), (k, "k"), (q_out, "q_out"), (k_out, "k_out")) if t is not None]
+    index = _on_device([t for t, _ in used], " ".join([n for _, n in used]))
     if transpose is not None and bool(transpose) != bool(rope.transpose):
         rope = Rope.from_buffer_copy(rope)
         rope.transpose = 1 if transpose else 0
@@ -257,7 +290,7 @@ def apack_rotary(pos, rope, q=None, k=None, q_out=None, k_out=None, transpose=No
     if q is not None:
         hq = _heads(q, "q", dtype)
         if q_out is None:
-            q_out = _new(stream, q.shape, dtype, q.device)
+            q_out = _like(stream, q)
         elif q_out.shape != q.shape:
             _fail(2, "q_out must have q's shape")
         hqo = _heads(q_out, "q_out", dtype)
@@ -266,7 +299,7 @@ def apack_rotary(pos, rope, q=None, k=None, q_out=None, k_out=None, transpose=No
         if k.shape[1:] != some.shape[1:]:
             _fail(2, "q and k must agree in rows and d")
         if k_out is None:
-            k_out = _new(stream, k.shape, dtype, k.device)
+            k_out = _like(stream, k)
         elif k_out.shape != k.shape:
             _fail(2, "k_out must have k's shape")
         hko = _heads(k_out, "k_out", dtype)
@@ -311,8 +344,8 @@ def apack_pages_copy(pairs, k_pages, v_pages=(), stream=None):
     """Copies page pairs[i, 0] to page pairs[i, 1] in every layer's K and V.
     pairs: int32 CUDA tensor [n, 2]; k_pages, v_pages: per layer [pages, heads,
     rows, d], or one tensor [layers, pages, heads, rows, d]."""
-    index = _on_device((pairs, "pairs"), (_first(k_pages, "k_pages"), "k_pages"),
-                       *([(_first(v_pages, "v_pages"), "v_pages")] if len(v_pages) else []))
+    first = _first(k_pages, "k_pages")
+    index = _on_device((pairs, first, _first(v_pages, "v_pages") if len(v_pages) else first), "pairs k_pages v_pages")
     p = _int32(pairs, "pairs", 2)
     if pairs.shape[1] != 2:
         _fail(2, "pairs must be [n, 2]")
@@ -329,14 +362,11 @@ def apack_compact_kv_pages(src_rows, seqs, k_in, v_in, k_out, v_out, table_in=No
     a side's tensors are [pages, heads, rows, d] per layer, without one [heads,
     rows, d]; a list of layers or one tensor with layers first."""
     n = len(seqs)
-    used = [(_first(k_in, "k_in"), "k_in"), (_first(k_out, "k_out"), "k_out")]
-    for x, name in ((v_in, "v_in"), (v_out, "v_out")):
-        if len(x):
-            used.append((_first(x, name), name))
-    for x, name in ((src_rows, "src_rows"), (table_in, "table_in"), (table_out, "table_out")):
-        if x is not None:
-            used.append((x, name))
-    index = _on_device(*used)
+    first = _first(k_in, "k_in")
+    index = _on_device((first, _first(k_out, "k_out"), _first(v_in, "v_in") if len(v_in) else first,
+                        _first(v_out, "v_out") if len(v_out) else first, first if src_rows is None else src_rows,
+                        first if table_in is None else table_in, first if table_out is None else table_out),
+                       "k_in k_out v_in v_out src_rows table_in table_out")
     moves = (Move * max(1, n))(*seqs)
     src = None
     if src_rows is not None:
@@ -355,17 +385,13 @@ def apack_rotary_append(pos, rope, q, k, v, k_pages, v_pages, table, lens, q_out
     if not given; it may be q)."""
     if q.dim() != 3:
         _fail(2, "q must be [hq, n_seq, d]")
-    index = _on_device((q, "q"), (pos, "pos"), (k, "k"), (v, "v"), (k_pages, "k_pages"), (v_pages, "v_pages"),
-                       (table, "table"), (lens, "lens"), (q if q_out is None else q_out, "q_out"))
+    index = _on_device((q, pos, k, v, k_pages, v_pages, table, lens, q if q_out is None else q_out),
+                       "q pos k v k_pages v_pages table lens q_out")
     _, n, d = q.shape
     dtype = q.dtype
     p, ps = _positions(pos, rope, n)
-    pages = _pages((k_pages,), (v_pages,), table, n)
+    pages = _one_layer(k_pages, v_pages, dtype, table, n, d)
     hq, hk, hv = _heads(q, "q", dtype), _heads(k, "k", dtype), _heads(v, "v", dtype)
-    if k_pages.dtype is not dtype:
-        _fail(3, "q and the pages must share a dtype")
-    if d != pages.d:
-        _fail(2, "q and the pages differ in d")
     shape = (pages.hkv, n, d)
     if k.shape != shape or v.shape != shape:
         _fail(2, f"k and v must be [{pages.hkv}, {n}, {d}]")
@@ -373,7 +399,7 @@ def apack_rotary_append(pos, rope, q, k, v, k_pages, v_pages, table, lens, q_out
     if lens.shape[0] != n:
         _fail(2, f"lens must be [{n}]")
     if q_out is None:
-        q_out = _new(stream, q.shape, dtype, q.device)
+        q_out = _like(stream, q)
     elif q_out.shape != q.shape:
         _fail(2, "q_out must have q's shape")
     _check(library().apack_rotary_append(rope, n, p, ps, lp, hq, _heads(q_out, "q_out", dtype), hk, hv, pages,
@@ -396,17 +422,13 @@ def apack_paged_attention(q, k_pages, v_pages, table, lens, max_len, mask=None, 
     torch = _torch()
     if q.dim() != 3:
         _fail(2, "q must be [hq, n_seq, d]")
-    index = _on_device((q, "q"), (k_pages, "k_pages"), (v_pages, "v_pages"), (table, "table"), (lens, "lens"),
-                       *[(t, n) for t, n in ((mask, "mask"), (out, "out"), (lse, "lse"), (workspace, "workspace"))
-                         if t is not None])
+    index = _on_device((q, k_pages, v_pages, table, lens, q if mask is None else mask, q if out is None else out,
+                        q if lse is None else lse, q if workspace is None else workspace),
+                       "q k_pages v_pages table lens mask out lse workspace")
     hq, n, d = q.shape
     dtype, max_len = q.dtype, int(max_len)
     qh = _heads(q, "q", dtype)
-    pages = _pages((k_pages,), (v_pages,), table, n)
-    if k_pages.dtype is not dtype:
-        _fail(3, "q and the pages must share a dtype")
-    if d != pages.d:
-        _fail(2, "q and the pages differ in d")
+    pages = _one_layer(k_pages, v_pages, dtype, table, n, d)
     lp = _int32(lens, "lens", 1)
     if lens.shape[0] != n:
         _fail(2, f"lens must be [{n}]")
@@ -420,7 +442,7 @@ def apack_paged_attention(q, k_pages, v_pages, table, lens, max_len, mask=None, 
     if scale is not None and not scale > 0:
         _fail(1, "scale must be > 0")
     if out is None:
-        out = _new(stream, q.shape, dtype, q.device)
+        out = _like(stream, q)
     elif out.shape != q.shape:
         _fail(2, "out must have q's shape")
     if return_lse and lse is None:

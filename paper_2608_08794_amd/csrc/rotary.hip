@@ -331,8 +331,9 @@ apack_status apack_rope_init(apack_rope* r, int32_t rot_dim, int32_t layout, dou
   r->pos_rows = 1;
   r->sections[0] = rot_dim / 2;
   r->factor = scaling == APACK_ROPE_SCALE_BY_PARTS ? 0.1 * std::log(s) + 1 : 1.0;
+  const double step = -2.0 * std::log(base) / rot_dim;
   for (int i = 0; i < rot_dim / 2; ++i) {
-    double f = std::pow(base, -2.0 * i / rot_dim);
+    double f = std::exp(i * step);
     if (scaling == APACK_ROPE_SCALE_LINEAR) f /= s;
     if (scaling == APACK_ROPE_SCALE_BY_PARTS) {
       const double turns = (double)trained_len * f / kTwoPi;
