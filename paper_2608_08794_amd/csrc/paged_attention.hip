@@ -607,10 +607,11 @@ int64_t plan(int64_t n_seq, int64_t items, int64_t span) {
   return std::min<int64_t>(kShares, (n_seq * items * tiles + kLeast - 1) / kLeast);
 }
 
-// Tiles of all sequences are counted in 32 bits, and times key heads and shares stay below 2^50.
+// Row numbers, up to a few thousand past max_len where steps are looked ahead, are 32-bit; tiles of all sequences
+// are counted in 32 bits, and times key heads and shares stay below 2^50.
 bool sizes_ok(int64_t n_seq, int32_t hq, int32_t hkv, int32_t d, int64_t max_len) {
   return n_seq >= 0 && n_seq < 65536 && hkv >= 1 && hkv < 256 && hq >= hkv && hq % hkv == 0 && hq < 4096 &&
-         (d == 64 || d == 128) && max_len >= 0 && max_len < (int64_t(1) << 31) - 64 &&
+         (d == 64 || d == 128) && max_len >= 0 && max_len <= (int64_t(1) << 31) - (1 << 16) &&
          n_seq * (max_len / kTile + 1) < (int64_t(1) << 31);
 }
 
