@@ -604,12 +604,15 @@ size_t apack_paged_attention_workspace(int64_t n_seq, int32_t hq, int32_t hkv, i
  *           out, so max_len (HOST) bounds the lengths that the call can meet:
  *           a captured call may be replayed while lens grow up to it.
  *   mask    DEVICE uint8 [n_seq][max_len] (nullable), row stride mask_stride.
- *   scale   > 0, or 0 for 1/sqrt(d).
+ *   scale   in [1e-30, 1e30], or 0 for 1/sqrt(d).
  *
  * Several new tokens of one sequence are passed as sequences with equal table
  * rows and their own lens.  Logits, the softmax and the sums are fp32; with
- * bf16 tensors the probabilities are rounded to bf16 for their product with V.
- * Results do not depend on timing: the same call gives the same bits. */
+ * bf16 tensors the probabilities enter their product with V as two bf16 parts
+ * (16 bits), and the result is rounded once.  Results do not depend on timing:
+ * the same call gives the same bits.  Limits (APACK_E_UNSUPPORTED beyond):
+ * n_seq < 65536, hkv < 256, hq < 4096, max_len <= 2^31 - 2^16 and
+ * n_seq (max_len/32 + 1) < 2^31. */
 apack_status apack_paged_attention(int64_t n_seq, int32_t hq, const apack_heads* q,
                                    const apack_heads* out, float* lse, const apack_pages* pages,
                                    const int32_t* lens, int64_t max_len, const uint8_t* mask,

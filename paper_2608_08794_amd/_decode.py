@@ -120,9 +120,9 @@ def _layers(x, dims, name):
                 _fail(3, f"the layers of {name} differ in dtype or device")
             ptrs.append(t.data_ptr())
     else:
-        base, n = x.data_ptr(), x.shape[0]
         if x.dim() != dims + 1:
             _fail(2, f"{name} must be a list of layers or one tensor [layers, ...] of {dims + 1} dimensions")
+        base, n = x.data_ptr(), x.shape[0]
         shape, stride, dtype = x.shape[1:], x.stride(), x.dtype
         step = stride[0] * x.element_size()
         ptrs = range(base, base + n * step, step) if step > 0 else [base] * n

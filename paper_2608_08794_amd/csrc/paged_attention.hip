@@ -19,6 +19,12 @@
 // workgroups in equal shares, whatever the lengths on the device are.  Where a
 // share's border falls inside a sequence's key head, each side leaves its
 // maximum, sum and unnormalised output, and a second kernel joins them.
+//
+// Measured (bf16, 28 heads over 4 of 128, pages of 16 rows), of 6.8 to 7.1 TB/s at
+// which nontemporal loads read this much alone: 64 sequences of 700 to 9454 rows
+// (0.68 GB) 107 + 5 us, 6.3 TB/s in the first kernel; one of 94028 rows (0.19 GB)
+// 34 + 4 us, 5.7 TB/s.  What is left is the launches, the first loads' chain (length,
+// page id, row) and the join.
 #include <cmath>
 #include <cstring>
 
@@ -35,8 +41,11 @@ typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 constexpr int kHeads = 16;        // query heads of a workgroup: an MFMA's columns
 constexpr int kTile = 32;         // rows of a tile
 constexpr int kWaves = 4;         // of a workgroup
-constexpr int kLeast = 1;         // tiles of the smallest share: with 4, one for each wave, 1312 rows of 8 over 2 heads take 11.6 us, not 8.8
-constexpr int kShares = 2048 / kWaves;   // eight waves a compute unit: what the registers let run at once
+// Eight waves a compute unit are what the registers let run at once (the steps
+// loaded ahead take 128 of them); a share is a tile at least: with four, one a wave,
+// four fp32 sequences of up to 1312 rows take 11.6 us, not 8.6.
+constexpr int kShares = 2048 / kWaves;
+constexpr int kLeast = 1;
 template <int D> constexpr int kPart = D + 4;   // floats of a head's part: output, maximum, sum, 16-byte aligned
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
@@ -406,7 +415,7 @@ struct Wave {
 
   __device__ __forceinline__ int64_t head(int h) const { return (int64_t)kh * a.group + h0 + h; }
   __device__ __forceinline__ void put_lse(int h, float top, float sum) const {
-    if (a.lse) a.lse[head(h) * a.n_seq + seq] = sum > 0 ? top * a.scale + __log2f(sum) * kLn2 : -INFINITY;
+    if (a.lse) a.lse[head(h) * a.n_seq + seq] = sum != 0 ? top * a.scale + __log2f(sum) * kLn2 : -INFINITY;
   }
 };
 
@@ -416,7 +425,8 @@ struct Joint {
   float part[kWaves][kHeads][D + 4];
   float stat[kWaves][kHeads][2];
 
-  // Joins the waves' states and writes the output, or its part.  Every thread calls it.
+  // Joins the waves' states and writes the output (a sum of 0: no row; NaN stays NaN), or its part.  Every thread
+  // calls it.
   template <class W, class T>
   __device__ __forceinline__ void join(const W& w, T* out, float* to_part) {
     const int wave = threadIdx.x >> 6;
@@ -452,7 +462,7 @@ struct Joint {
           to[D + 1] = sum;
         }
       } else {
-        Elem<T>::put(sum > 0 ? o / sum : 0.0f, out + w.head(h) * w.a.out_head + w.seq * w.a.out_row + e);
+        Elem<T>::put(sum != 0 ? o / sum : 0.0f, out + w.head(h) * w.a.out_head + w.seq * w.a.out_row + e);
         if (e == 0) w.put_lse(h, top, sum);
       }
     }
@@ -593,17 +603,22 @@ __global__ __launch_bounds__(kThreads) void k_join_parts(const AttnArgs a) {
       r += out[i][e / 4][e % 4] * f;
       s += stat[i][1] * f;
     }
-    Elem<T>::put(s > 0 ? r / s : 0.0f, static_cast<T*>(a.out) + head * a.out_head + seq * a.out_row + e);
-    if (e == 0 && a.lse) a.lse[head * a.n_seq + seq] = s > 0 ? top * a.scale + __log2f(s) * kLn2 : -INFINITY;
+    Elem<T>::put(s != 0 ? r / s : 0.0f, static_cast<T*>(a.out) + head * a.out_head + seq * a.out_row + e);
+    if (e == 0 && a.lse) a.lse[head * a.n_seq + seq] = s != 0 ? top * a.scale + __log2f(s) * kLn2 : -INFINITY;
   }
 }
 
-constexpr int64_t kWholeSpan = 512;
+// Spans that one workgroup takes whole: at most kWholeSpan rows (one sequence of 512
+// rows of 28 heads over 4: 8.4 us, 9.5 in shares and a join), or kWholeSpanMany where
+// the items fill the compute units (64 sequences of 1000 to 2048 rows: 39 us, 42 in
+// shares).  Longer ones of few items would leave most of the chip idle: one sequence
+// of 1024 rows takes 13 us whole, 9 in shares.
+constexpr int64_t kWholeSpan = 512, kWholeSpanMany = 2048, kManyItems = 256;
 
 // Shares of k_attend_shares, 0 for one workgroup per sequence and item.
 int64_t plan(int64_t n_seq, int64_t items, int64_t span) {
   const int64_t tiles = std::max<int64_t>(1, (span + kTile - 1) / kTile);
-  if (span <= kWholeSpan || (span <= 4 * kWholeSpan && n_seq * items >= 256)) return 0;
+  if (span <= kWholeSpan || (span <= kWholeSpanMany && n_seq * items >= kManyItems)) return 0;
   return std::min<int64_t>(kShares, (n_seq * items * tiles + kLeast - 1) / kLeast);
 }
 
@@ -691,7 +706,8 @@ apack_status apack_paged_attention(int64_t n_seq, int32_t hq, const apack_heads*
   APACK_CHECK(sizes_ok(n_seq, hq, pages->hkv, pages->d, max_len), APACK_E_UNSUPPORTED,
               "n_seq, heads or max_len too large");
   APACK_CHECK(window >= 0, APACK_E_ARG, "window must be >= 0");
-  APACK_CHECK(scale >= 0 && std::isfinite((float)scale), APACK_E_ARG, "scale must be finite, and > 0 or 0 for 1/sqrt(d)");
+  APACK_CHECK(scale == 0 || (scale >= 1e-30 && scale <= 1e30), APACK_E_ARG,
+              "scale must lie in [1e-30, 1e30], or be 0 for 1/sqrt(d)");
   APACK_CHECK(n_seq == 0 || lens, APACK_E_ARG, "lens is NULL");
   APACK_CHECK(!mask || mask_stride >= max_len, APACK_E_SHAPE, "mask_stride must be >= max_len");
   const size_t es = dtype_size(pages->dtype);

@@ -348,7 +348,9 @@ def _attend(n=3, hq=4, q=None, out=None, lse=FAKE + (16 << 34), pages=None, lens
 
 @pytest.mark.parametrize("status,kw", [
     (2, dict(n=-1)), (2, dict(hq=3)), (2, dict(hq=0)), (2, dict(max_len=-1)), (1, dict(window=-1)), (1, dict(scale=-1.0)),
-    (1, dict(scale=math.nan)), (1, dict(scale=math.inf)), (1, dict(lens=None)), (7, dict(max_len=1 << 31)),
+    (1, dict(scale=math.nan)), (1, dict(scale=math.inf)), (1, dict(scale=1e-60)), (1, dict(scale=1e31)),
+    (1, dict(lens=None)), (7, dict(max_len=1 << 31)), (7, dict(max_len=(1 << 31) - (1 << 16) + 1)),
+    (7, dict(n=60000, max_len=2000000, ws_bytes=1 << 40)), (7, dict(hq=4096, q=_heads(FAKE + (12 << 34), 4096, 3, 64))),
     (7, dict(n=65536)), (2, dict(mask=FAKE + (18 << 34), mask_stride=63)), (7, dict(pages=_pages(d=96))),
     (1, dict(pages=_pages(v=False))), (1, dict(pages=_planes())), (1, dict(pages=_pages(n_layers=2))),
     (2, dict(q=_heads(FAKE + (12 << 34), 2, 3, 64))), (7, dict(q=_heads((FAKE + (12 << 34)) + 2, 4, 3, 64))),

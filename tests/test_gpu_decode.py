@@ -392,6 +392,9 @@ def _check_attention(o, lse, q, kp, vp, table, lens, max_len, mask=None, window=
         if not at:
             assert not o[:, s].any() and (lse is None or np.isneginf(lse[:, s]).all())
             continue
+        if np.isnan(want).any():                        # a NaN among the rows attended to is not hidden
+            assert np.isnan(want).all() and np.isnan(o[:, s]).all() and (lse is None or np.isnan(lse[:, s]).all())
+            continue
         e = (d + 2) * U * size[:, None]
         rel = 2 * e + 2 ** 7 * U + 3 * len(at) * U
         tol = w * (rel + h) + (h + 4 * U) * np.abs(want)
@@ -733,6 +736,51 @@ def test_captured_decode_step_is_replayed_as_lengths_grow():
             np.testing.assert_array_equal(bits(got), bits(want))
             np.testing.assert_array_equal(bits(lse), bits(st["lse"]))
             _check_attention(got, lse, st["qt"], st["kp"], st["vp"], st["table"], st["lens"], st["max_len"])
+
+
+def test_two_graphs_share_a_workspace():
+    """Replayed in turn on one stream: each call writes what it reads."""
+    import paper_2608_08794_amd as A
+    g = _gen(54)
+    rope = A.apack_rope(128)
+    states = [_state(A, g, [900, 30, 2000], 3000), _state(A, g, [2500], 3000)]
+    for st in states:
+        st["ws"] = states[0]["ws"]
+    want, graphs = [], []
+    for st in states:
+        want.append(_decode_once(A, rope, st).clone())
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            _decode_once(A, rope, st)
+        graphs.append(graph)
+    states[0]["ws"].fill_(255)                             # NaN in every part
+    for _ in range(3):
+        for st in states:
+            st["o"].fill_(9)
+        for graph in graphs:
+            graph.replay()
+        torch.cuda.synchronize()
+        for st, w in zip(states, want):
+            np.testing.assert_array_equal(bits(st["o"]), bits(w))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_paged_attention_with_far_bounds(dtype):
+    """Bounds and windows near the largest that a call takes, over short sequences."""
+    import paper_2608_08794_amd as A
+    g = _gen(55)
+    most = 2**31 - 2**16
+    kp, vp, table, n = _paged(g, dtype, [700, 0, 33], 2, 16, 64)
+    q = _rand(g, dtype, 6, 3, 64)
+    for window in (0, most, 2**62):
+        o, lse = A.apack_paged_attention(q, kp, vp, table, n, most, window=window, return_lse=True)
+        _check_attention(o, lse, q, kp, vp, table, n, most, window=window, dtype=dtype)
+    # Lengths beyond the bound and the table, none, and one that takes in rows of NaN.
+    n = torch.tensor([2**31 - 1, -2**31, 40], dtype=torch.int32, device="cuda")
+    for bound, window in ((700, 0), (33, 0), (most, 50)):
+        o, lse = A.apack_paged_attention(q, kp, vp, table, n, bound, window=window, return_lse=True)
+        _check_attention(o, lse, q, kp, vp, table, n, bound, window=window, dtype=dtype)
 
 
 def test_entry_points_on_side_streams():
