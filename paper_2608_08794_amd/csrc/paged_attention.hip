@@ -742,8 +742,9 @@ apack_status apack_paged_attention(int64_t n_seq, int32_t hq, const apack_heads*
   pk.data = pages->k[0];
   pv.data = pages->v[0];
   const Strided reads[] = {tq, pk, pv, range(lens, (size_t)n_seq * 4),
-                           range(pages->table, (size_t)((n_seq - 1) * pages->table_stride + pages->table_width) * 4),
-                           range(mask, mask ? (size_t)((n_seq - 1) * mask_stride + max_len) : 0)};
+                           rows_of_stride(pages->table, 4, n_seq, pages->table_stride, pages->table_width),
+                           rows_of_stride(mask, 1, n_seq, mask_stride, max_len)};
+  for (const Strided& r : reads) APACK_CHECK(r.ok, APACK_E_SHAPE, "a table or mask of 2^46 elements or more");
   const Strided writes[] = {to, range(lse, lse ? (size_t)hq * n_seq * 4 : 0), range(ws, need)};
   for (int i = 0; i < 3; ++i) {
     for (const Strided& r : reads) APACK_CHECK(apart(writes[i], r), APACK_E_ALIAS, "an output or the workspace overlaps an input");

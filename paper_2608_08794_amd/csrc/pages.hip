@@ -299,6 +299,7 @@ apack_status apack_pages_copy(const apack_pages* pages, int64_t n_pairs, const i
   apack_status st = check_pages(pages, "pages", &dev, &plane);
   if (st != APACK_OK) return st;
   APACK_CHECK(n_pairs >= 0, APACK_E_ARG, "n_pairs must be >= 0");
+  APACK_CHECK(n_pairs < (int64_t(1) << 31), APACK_E_UNSUPPORTED, "n_pairs must be < 2^31");
   APACK_CHECK(n_pairs == 0 || pairs, APACK_E_ARG, "pairs is NULL");
   const int64_t es = (int64_t)dtype_size(pages->dtype);
   for (int l = 0; l < pages->n_layers; ++l)
@@ -334,8 +335,8 @@ apack_status apack_pages_copy(const apack_pages* pages, int64_t n_pairs, const i
   a.stride0 = dim[0][0] * es / ub;
   a.stride1 = dim[1][0] * es / ub;
   const int64_t slabs = (a.page_units + kThreads - 1) / kThreads;
-  APACK_CHECK(a.page_units + kThreads < (int64_t(1) << 31) && slabs * n_pairs < (int64_t(1) << 31), APACK_E_UNSUPPORTED,
-              "pages of 2^31 units, or that many slabs of them");
+  APACK_CHECK(a.page_units + kThreads < (int64_t(1) << 31) && n_pairs < kMaxThreads / kThreads / slabs,
+              APACK_E_UNSUPPORTED, "2^31 units of %d bytes in a page, or 2^32 in one layer's pages copied", (int)ub);
   a.slabs = (int32_t)slabs;
   a.by_run = FastDiv((uint32_t)a.run);
   a.by_count0 = FastDiv((uint32_t)dim[0][1]);
@@ -403,10 +404,9 @@ apack_status apack_compact_kv_pages(int32_t n_seq, const apack_move* seqs, const
     return fail(APACK_E_HIP, "out of host memory");
   }
   const Strided kept = range(src_rows, (size_t)(src_rows ? total : 0) * 4);
-  auto table_of = [&](const apack_pages* p) {
-    return range(p->table, p->table && n_seq ? (size_t)((n_seq - 1) * p->table_stride + p->table_width) * 4 : 0);
-  };
-  const Strided t_in = table_of(in), t_out = table_of(out);
+  const Strided t_in = rows_of_stride(in->table, 4, n_seq, in->table_stride, in->table_width);
+  const Strided t_out = rows_of_stride(out->table, 4, n_seq, out->table_stride, out->table_width);
+  APACK_CHECK(t_in.ok && t_out.ok, APACK_E_SHAPE, "a table of 2^46 entries or more");
   for (size_t i = 0; i < outs.size(); ++i) {
     const Strided o = at(tout, outs[i]);
     APACK_CHECK(apart(o, kept) && apart(o, t_in) && apart(o, t_out), APACK_E_ALIAS,

@@ -15,6 +15,7 @@
 namespace apack {
 
 constexpr int kMaxLayers = 64;
+constexpr int64_t kMaxThreads = int64_t(1) << 32;   // threads of a launch's first dimension, exclusive
 
 // n / d for 0 <= n < 2^31 and 1 <= d < 2^31 as (n * m) >> (31 + s) with
 // s = ceil(log2 d) and m = ceil(2^(31+s) / d) < 2^32: m*d exceeds 2^(31+s) by
@@ -82,6 +83,11 @@ inline bool apart(const Strided& a, const Strided& b) {
 
 // A contiguous range as a Strided.
 inline Strided range(const void* data, size_t bytes) { return strided(data, 1, (int64_t)bytes, {}); }
+
+// `rows` rows of `width` elements at a stride (host checks of tables, masks, position ids).
+inline Strided rows_of_stride(const void* data, size_t es, int64_t rows, int64_t stride, int64_t width) {
+  return data && rows ? strided(data, es, width, {{stride, rows}}) : range(data, 0);
+}
 
 // Addressing of a pool (one page that holds the packed rows without a table).
 struct PoolDev {

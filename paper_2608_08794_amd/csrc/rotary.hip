@@ -277,7 +277,7 @@ apack_status run(RotaryArgs& a, const apack_rope* rope, apack_dtype dtype, bool 
   a.chunk_magic = (65536 + a.chunks - 1) / a.chunks;
   a.rows_per_wg = kThreads / a.chunks;
   const int64_t blocks = (a.rows + a.rows_per_wg - 1) / a.rows_per_wg;
-  APACK_CHECK(blocks < (int64_t(1) << 31), APACK_E_UNSUPPORTED, "too many rows");
+  APACK_CHECK(blocks < kMaxThreads / kThreads, APACK_E_UNSUPPORTED, "too many rows of %d elements for one call", a.d);
   // Heads are split over workgroups until there are 1024 of them, and to two a
   // thread where vectors of it are in flight: 94028 rows of 32 heads of 128 take 261 us
   // so, 275 with eight heads a thread; single elements take 84 us for 20000 rows with
@@ -358,7 +358,6 @@ apack_status apack_rotary(const apack_rope* rope, int64_t rows, const int32_t* p
   APACK_CHECK(rows < (int64_t(1) << 31), APACK_E_UNSUPPORTED, "rows must be < 2^31");
   APACK_CHECK(rows == 0 || pos, APACK_E_ARG, "pos is NULL");
   APACK_CHECK(rope->pos_rows == 1 || pos_stride >= rows, APACK_E_SHAPE, "pos_stride must be >= rows");
-  APACK_CHECK(pos_stride < (int64_t(1) << 46), APACK_E_UNSUPPORTED, "pos_stride must be < 2^46");
   APACK_CHECK(!q_in == !q_out && !k_in == !k_out, APACK_E_ARG, "an input without its output, or the reverse");
   const size_t es = dtype_size(dtype);
   Strided ins[2], outs[2];
@@ -373,7 +372,8 @@ apack_status apack_rotary(const apack_rope* rope, int64_t rows, const int32_t* p
     APACK_CHECK(in[i]->heads == out[i]->heads, APACK_E_SHAPE, "%s and %s differ in heads", names[i][0], names[i][1]);
     a.t[i] = dev_heads(in[i], out[i]);
   }
-  const Strided p = range(pos, rows ? (size_t)((rope->pos_rows - 1) * pos_stride + rows) * 4 : 0);
+  const Strided p = rows_of_stride(rows ? pos : nullptr, 4, rope->pos_rows, pos_stride, rows);
+  APACK_CHECK(p.ok, APACK_E_SHAPE, "pos of 2^46 elements or more");
   for (int i = 0; i < 2; ++i) {
     if (!out[i]) continue;
     APACK_CHECK(apart(outs[i], p), APACK_E_ALIAS, "%s overlaps pos", names[i][1]);
@@ -407,7 +407,6 @@ apack_status apack_rotary_append(const apack_rope* rope, int64_t n_seq, const in
   APACK_CHECK(n_seq < (int64_t(1) << 31), APACK_E_UNSUPPORTED, "n_seq must be < 2^31");
   APACK_CHECK(n_seq == 0 || (pos && lens), APACK_E_ARG, "pos or lens is NULL");
   APACK_CHECK(rope->pos_rows == 1 || pos_stride >= n_seq, APACK_E_SHAPE, "pos_stride must be >= n_seq");
-  APACK_CHECK(pos_stride < (int64_t(1) << 46), APACK_E_UNSUPPORTED, "pos_stride must be < 2^46");
   const size_t es = dtype_size(pages->dtype);
   Strided ins[3], qo;
   const apack_heads* const in[3] = {q_in, k, v};
@@ -423,9 +422,10 @@ apack_status apack_rotary_append(const apack_rope* rope, int64_t n_seq, const in
   Strided pk = plane, pv = plane;
   pk.data = pages->k[0];
   pv.data = pages->v[0];
-  const Strided reads[3] = {range(pos, n_seq ? (size_t)((rope->pos_rows - 1) * pos_stride + n_seq) * 4 : 0),
+  const Strided reads[3] = {rows_of_stride(n_seq ? pos : nullptr, 4, rope->pos_rows, pos_stride, n_seq),
                             range(lens, (size_t)n_seq * 4),
-                            range(pages->table, n_seq ? (size_t)((n_seq - 1) * pages->table_stride + pages->table_width) * 4 : 0)};
+                            rows_of_stride(pages->table, 4, n_seq, pages->table_stride, pages->table_width)};
+  APACK_CHECK(reads[0].ok && reads[2].ok, APACK_E_SHAPE, "pos or a table of 2^46 elements or more");
   for (const Strided& o : {qo, pk, pv}) {
     for (const Strided& r : reads) APACK_CHECK(apart(o, r), APACK_E_ALIAS, "an output overlaps pos, lens or the table");
     for (int i = 0; i < 3; ++i) {

@@ -224,6 +224,7 @@ NAN_FREQ = (ctypes.c_double * 128)(*([math.nan] * 128))
     (2, dict(rope=_rope(sections=(ctypes.c_int32 * 4)(31, 0, 0, 0)))),
     (2, dict(rope=_rope(pos_rows=2, sections=(ctypes.c_int32 * 4)(33, -1, 0, 0)))),
     (2, dict(rope=_rope(pos_rows=2, sections=(ctypes.c_int32 * 4)(16, 16, 0, 0)), stride=7)),
+    (2, dict(rope=_rope(pos_rows=3, sections=(ctypes.c_int32 * 4)(16, 8, 8, 0)), stride=1 << 61)),
     (1, dict(rope=_rope(factor=math.inf))), (1, dict(rope=_rope(factor=1e300))), (1, dict(rope=_rope(freq=NAN_FREQ))),
     (2, dict(q=_heads(FAKE, 0, 8, 64))), (1, dict(q=_heads(None, 4, 8, 64))), (1, dict(q=_heads(FAKE, 4, 8, 64, reserved=1))),
     (2, dict(q=_heads(FAKE, 4, 8, 64, row_stride=63))), (2, dict(q=_heads(FAKE, 4, 8, 64, head_stride=0))),
@@ -239,6 +240,13 @@ NAN_FREQ = (ctypes.c_double * 128)(*([math.nan] * 128))
 def test_rotary_refusals(status, kw):
     st, msg = _rotary(**kw)
     assert st == status and msg
+
+
+def test_rotary_of_more_rows_than_one_launch_takes():
+    far = FAKE << 12                                          # rows of 511 single elements, one a workgroup
+    st, msg = _rotary(rows=1 << 25, stride=1 << 25, d=511, pos=FAKE, q=_heads(far, 1, 1 << 25, 511),
+                      qo=_heads(far << 1, 1, 1 << 25, 511))
+    assert st == 7 and "too many rows" in msg
 
 
 def test_rotary_of_no_rows_does_nothing():
@@ -264,7 +272,8 @@ def test_copy_refusals():
     assert _status("apack_pages_copy", _pages(), 1, None, None)[0] == 1
     assert _status("apack_pages_copy", _pages(), 1, FAKE + 16, None)[0] == 5
     assert _status("apack_pages_copy", _pages(), 0, None, None)[0] == 0
-    assert _status("apack_pages_copy", _pages(), 1 << 31, FAKE + (8 << 34), None)[0] == 7
+    for pairs in (1 << 31, 1 << 24, 1 << 62):                # more threads than one launch takes
+        assert _status("apack_pages_copy", _pages(k0=FAKE << 8, v0=(FAKE << 8) + (1 << 34)), pairs, FAKE, None)[0] == 7
 
 
 def _compact(seqs, src=FAKE + (8 << 34), pin=None, pout=None):
@@ -295,6 +304,7 @@ OUT = dict(k0=FAKE + (3 << 34), v0=FAKE + (4 << 34))
     (5, [(0, 4, 0, 2)], dict(pout=_pages(k0=FAKE + (3 << 34), v0=FAKE + (3 << 34)))),
     (5, [(0, 4, 0, 2)], dict(src=FAKE + (3 << 34) + 4)),
     (5, [(0, 4, 0, 2)], dict(pout=_pages(table=FAKE + (3 << 34), **OUT))),
+    (2, [(0, 4, 0, 2)] * 2, dict(pin=_pages(table_stride=1 << 62))),
 ])
 def test_compact_pages_refusals(status, seqs, kw):
     st, msg = _compact(seqs, **kw)
@@ -332,6 +342,7 @@ def _append(n=3, pos=FAKE + (10 << 34), lens=FAKE + (11 << 34), q=None, qo=None,
     (5, dict(qo=_heads(FAKE, 4, 3, 64))), (5, dict(k=_heads(FAKE + 64, 2, 3, 64))), (5, dict(lens=FAKE + 4)),
     (5, dict(qo=_heads(FAKE + (11 << 34), 4, 3, 64))), (5, dict(qo=_heads(FAKE + (12 << 34) + 64, 4, 3, 64))),
     (5, dict(v=_heads(FAKE + (13 << 34), 2, 3, 64))), (5, dict(pages=_pages(table=FAKE + 8))),
+    (2, dict(pages=_pages(table_stride=1 << 61))),
 ])
 def test_append_refusals(status, kw):
     st, msg = _append(**kw)
@@ -351,7 +362,8 @@ def _attend(n=3, hq=4, q=None, out=None, lse=FAKE + (16 << 34), pages=None, lens
     (1, dict(scale=math.nan)), (1, dict(scale=math.inf)), (1, dict(scale=1e-60)), (1, dict(scale=1e31)),
     (1, dict(lens=None)), (7, dict(max_len=1 << 31)), (7, dict(max_len=(1 << 31) - (1 << 16) + 1)),
     (7, dict(n=60000, max_len=2000000, ws_bytes=1 << 40)), (7, dict(hq=4096, q=_heads(FAKE + (12 << 34), 4096, 3, 64))),
-    (7, dict(n=65536)), (2, dict(mask=FAKE + (18 << 34), mask_stride=63)), (7, dict(pages=_pages(d=96))),
+    (7, dict(n=65536)), (2, dict(pages=_pages(table_stride=1 << 61))), (2, dict(mask=FAKE + (18 << 34), mask_stride=1 << 62)),
+    (2, dict(mask=FAKE + (18 << 34), mask_stride=63)), (7, dict(pages=_pages(d=96))),
     (1, dict(pages=_pages(v=False))), (1, dict(pages=_planes())), (1, dict(pages=_pages(n_layers=2))),
     (2, dict(q=_heads(FAKE + (12 << 34), 2, 3, 64))), (7, dict(q=_heads((FAKE + (12 << 34)) + 2, 4, 3, 64))),
     (7, dict(pages=_pages(row_stride=68, head_stride=16 * 68, page_stride=2 * 16 * 68))),
