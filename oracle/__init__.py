@@ -5,7 +5,7 @@ execute this package: only the tests, the smoke check and the benchmark's CPU
 baseline leg use it.  It shares no code with the HIP library or its Python
 binding, and it never receives a value computed by them.
 
-Two modules, one per half of the method:
+Two modules, one per half of the method, and one beside them:
 
 * ``oracle.prune``    -- the in-LLM query-conditioned prune (Section 3.2,
   Eq. 5 and Eq. 6; the inner loop of Algorithm 1): attention mass of the
@@ -15,6 +15,8 @@ Two modules, one per half of the method:
   (Section 3.1, Eq. 1-4; the first loop of Algorithm 1; the pre-LLM
   compression details of the supplement): frame pooling, windowed CKA, the
   gate, segmentation, budgets and anchor / non-anchor token selection.
+* ``oracle.decode``   -- rotary positions, a paged cache and one token's
+  attention over it (what a decoder does around the prune).
 
 Every floating-point step is binary64.  Inputs are the exact values of the
 bf16 or fp32 bit patterns, widened to fp64 by :func:`widen`.

@@ -109,7 +109,7 @@ void launch_copy(const CopyArgs& a, dim3 grid, hipStream_t s) {
 // ---------------------------------------------------------------------------
 
 constexpr int kMaxMoves = 48;   // sequences per launch (they travel as an argument)
-constexpr int kManyPlanes = 4;  // planes of a thread that copies several
+constexpr int kPlanes = 4;      // planes of a thread
 
 struct MoveArgs {
   const int32_t* kept;
@@ -138,8 +138,11 @@ __device__ __forceinline__ int64_t row_offset(const PoolDev& p, int seq, int64_t
 // Each thread finds where its unit comes from and goes to (the lanes of a row
 // read the same words: no LDS, no barrier) and copies it in kPlanes planes (layer
 // x {K, V} x head), whose rows lie alike.  All loads come before the stores: they
-// complete in order, so a load after a store would wait for it.
-template <class U, int kPlanes>
+// complete in order, so a load after a store would wait for it.  47014 of 94028 rows
+// of 28 layers, 5.4 GB: 961 us between pages in random order, 893 in ascending order
+// (6.0 TB/s); with one plane a thread 1576 (the look-ups' chain), with eight loaded
+// ahead of stores 1003.
+template <class U>
 __global__ __launch_bounds__(kThreads) void k_move_rows(const MoveArgs a) {
   const uint32_t u = blockIdx.x * (uint32_t)kThreads + threadIdx.x;   // < 2^31
   const int row = (int)a.by_units.div(u);
@@ -175,10 +178,10 @@ __global__ __launch_bounds__(kThreads) void k_move_rows(const MoveArgs a) {
   }
 }
 
-template <class U, int kPlanes>
+template <class U>
 void launch_move(const MoveArgs& a, unsigned blocks, hipStream_t s) {
   const dim3 grid(blocks, (unsigned)((a.planes + kPlanes - 1) / kPlanes));
-  hipLaunchKernelGGL((k_move_rows<U, kPlanes>), grid, dim3(kThreads), 0, s, a);
+  hipLaunchKernelGGL(k_move_rows<U>, grid, dim3(kThreads), 0, s, a);
 }
 
 inline void to_units(PoolDev& p, int64_t es, int64_t ub) {
@@ -457,12 +460,9 @@ apack_status apack_compact_kv_pages(int32_t n_seq, const apack_move* seqs, const
     done += rows;
     if (rows == 0) continue;
     const int64_t blocks = (rows * a.row_units + kThreads - 1) / kThreads;
-    // Planes share a thread's addresses where that leaves enough workgroups.
-    const bool many = blocks * planes >= kManyPlanes * 1024;
-    const unsigned n = (unsigned)blocks;
-    if (ub == 16) many ? launch_move<u32x4, kManyPlanes>(a, n, hs) : launch_move<u32x4, 1>(a, n, hs);
-    else if (ub == 4) many ? launch_move<uint32_t, kManyPlanes>(a, n, hs) : launch_move<uint32_t, 1>(a, n, hs);
-    else many ? launch_move<uint16_t, kManyPlanes>(a, n, hs) : launch_move<uint16_t, 1>(a, n, hs);
+    if (ub == 16) launch_move<u32x4>(a, (unsigned)blocks, hs);
+    else if (ub == 4) launch_move<uint32_t>(a, (unsigned)blocks, hs);
+    else launch_move<uint16_t>(a, (unsigned)blocks, hs);
     st = launch_status("k_move_rows");
     if (st != APACK_OK) return st;
   }
