@@ -575,9 +575,10 @@ apack_status apack_compact_kv_pages(int32_t n_seq, const apack_move* seqs, const
  * layer 0 of `pages` (one layer, with v and a table of n_seq rows).  lens is a
  * DEVICE int32 [n_seq] array of the lengths that include the new token.  A
  * sequence whose row is negative, beyond the table or in no page writes no k
- * and v; its q is turned.  Sequences must not share the page that they write
- * to.  q_out may be q_in; otherwise outputs overlap no inputs
- * (APACK_E_ALIAS). */
+ * and v; its q is turned.  No two sequences may write the same row: a forked
+ * one has to have its own last page, and several new tokens of one sequence are
+ * passed as sequences with equal table rows and increasing lens.  q_out may be
+ * q_in; otherwise outputs overlap no inputs (APACK_E_ALIAS). */
 apack_status apack_rotary_append(const apack_rope* rope, int64_t n_seq, const int32_t* pos,
                                  int64_t pos_stride, const int32_t* lens, const apack_heads* q_in,
                                  const apack_heads* q_out, const apack_heads* k,

@@ -687,6 +687,42 @@ def test_prune_compact_fork_and_decode():
     assert not refs.any()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_several_new_tokens_of_one_sequence(dtype):
+    """Four tokens of one sequence and two of another in one call of each, tables as columns of a wider one."""
+    import paper_2608_08794_amd as A
+    g = _gen(61)
+    kp, vp = (_rand(g, dtype, 9, 2, 16, 64) for _ in range(2))
+    wide = torch.full((6, 11), 77, dtype=torch.int32, device="cuda")
+    table = wide[:, 2:6]
+    table.copy_(torch.tensor([[3, 1, 8, -1]] * 4 + [[0, 5, 2, 4]] * 2, dtype=torch.int32))
+    lens = torch.tensor([15, 16, 17, 18, 50, 51], dtype=torch.int32, device="cuda")
+    q, k, v = (_rand(g, dtype, h, 6, 64) for h in (8, 2, 2))
+    rope = A.apack_rope(64, layout="interleaved")
+    k0, v0 = kp.clone(), vp.clone()
+    qt = A.apack_rotary_append(lens, rope, q, k, v, kp, vp, table, lens)
+    _, kt = A.apack_rotary(lens, rope, q, k)
+    for s, n in enumerate(lens.tolist()):
+        page, row = OD.place(table[s].tolist(), 16, n - 1, 9)
+        k0[page, :, row], v0[page, :, row] = kt[:, s], v[:, s]
+    assert torch.equal(kp, k0) and torch.equal(vp, v0)
+    o, lse = A.apack_paged_attention(qt, kp, vp, table, lens, 64, return_lse=True)
+    _check_attention(o, lse, qt, kp, vp, table, lens, 64, dtype=dtype)
+
+
+def test_calls_of_no_rows():
+    import paper_2608_08794_amd as A
+    rope = A.apack_rope(64)
+    none = torch.empty(0, dtype=torch.int32, device="cuda")
+    x = torch.empty(4, 0, 64, device="cuda")
+    q, k = A.apack_rotary(none, rope, x, x[:2])
+    assert q.shape == (4, 0, 64) and k.shape == (2, 0, 64)
+    p = torch.ones(1, 3, 2, 16, 64, device="cuda")
+    A.apack_compact_kv_pages(none, [(0, 5, 0, 0)], p, [], torch.zeros(1, 2, 7, 64, device="cuda"), [],
+                             table_in=torch.zeros(1, 1, dtype=torch.int32, device="cuda"))
+    assert (p == 1).all()
+
+
 def _decode_once(A, rope, st):
     qt = A.apack_rotary_append(st["pos"], rope, st["q"], st["k"], st["v"], st["kp"], st["vp"], st["table"], st["lens"],
                                q_out=st["qt"])
