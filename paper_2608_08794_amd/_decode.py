@@ -1,6 +1,7 @@
 """ctypes binding of the rotary, paged-cache and decode calls of include/apack.h
 (argument marshalling only)."""
 
+import array
 import ctypes
 
 from . import _lib
@@ -25,8 +26,8 @@ class Heads(ctypes.Structure):
 class Pages(ctypes.Structure):
     _fields_ = [("n_layers", _I32), ("n_pages", _I32), ("page_rows", _I32), ("hkv", _I32), ("d", _I32),
                 ("table_width", _I32), ("dtype", ctypes.c_int), ("reserved", _I32), ("page_stride", _I64),
-                ("head_stride", _I64), ("row_stride", _I64), ("k", ctypes.POINTER(_P)), ("v", ctypes.POINTER(_P)),
-                ("table", _P), ("table_stride", _I64)]
+                ("head_stride", _I64), ("row_stride", _I64), ("k", _P), ("v", _P), ("table", _P),
+                ("table_stride", _I64)]
 
 
 class Move(ctypes.Structure):
@@ -106,7 +107,7 @@ def _first(x, name):
     return x
 
 
-def _layers(x, dims, name):
+def _pointers(x, dims, name):
     """(pointers, shape, strides, dtype) of a tensor per layer: a list of them, or one tensor whose first dimension is
     the layer."""
     if isinstance(x, (list, tuple)):
@@ -122,37 +123,42 @@ def _layers(x, dims, name):
     else:
         if x.dim() != dims + 1:
             _fail(2, f"{name} must be a list of layers or one tensor [layers, ...] of {dims + 1} dimensions")
-        base, n = x.data_ptr(), x.shape[0]
-        shape, stride, dtype = x.shape[1:], x.stride(), x.dtype
-        step = stride[0] * x.element_size()
+        n, stride, dtype = x.shape[0], x.stride(), x.dtype
+        shape, step, stride = x.shape[1:], stride[0], stride[1:]
+        base, step = x.data_ptr(), step * x.element_size()
         ptrs = range(base, base + n * step, step) if step > 0 else [base] * n
-        stride = stride[1:]
     if len(shape) != dims:
         _fail(2, f"the layers of {name} must have {dims} dimensions")
     if stride[-1] != 1 and shape[-1] > 1:
         _fail(2, f"{name} must have contiguous elements")
-    return ptrs, shape, stride, dtype
+    return array.array("Q", ptrs), shape, stride, dtype
+
+
+def _given(v):
+    """Whether there is a V beside the K: a tensor, or a list that is not empty."""
+    return v is not None and (not isinstance(v, (list, tuple)) or len(v) > 0)
 
 
 def _pages(k, v, table=None, n_seq=0, name="pages", planes=False):
     """An apack_pages of [pages, heads, rows, d] tensors, or of planes [heads, rows, d]."""
     dims = 3 if planes else 4
-    ptrs, shape, stride, dtype = _layers(k, dims, f"k_{name}")
-    n = len(ptrs)
-    kp, vp = (_P * n)(*ptrs), None
-    if v is not None and len(v):
-        ptrs, vshape, vstride, vdtype = _layers(v, dims, f"v_{name}")
-        if len(ptrs) != n or vshape != shape or vstride != stride:
+    kp, shape, stride, dtype = _pointers(k, dims, f"k_{name}")
+    vp = None
+    if _given(v):
+        vp, vshape, vstride, vdtype = _pointers(v, dims, f"v_{name}")
+        if len(vp) != len(kp) or vshape != shape or vstride != stride:
             _fail(2, f"v_{name} must match k_{name} in layers, shape and strides")
         if vdtype is not dtype:
             _fail(3, f"v_{name} must match k_{name} in dtype")
-        vp = (_P * n)(*ptrs)
     if planes:
         pages, (hkv, rows, d), (sh, sr, _), sp = 1, shape, stride, 0
     else:
         (pages, hkv, rows, d), (sp, sh, sr, _) = shape, stride
     tp, width, ts = (None, 0, 0) if table is None else _table(table, n_seq)
-    return Pages(n, pages, rows, hkv, d, width, _code(dtype), 0, sp, sh, sr, kp, vp, tp, ts)
+    p = Pages(len(kp), pages, rows, hkv, d, width, _code(dtype), 0, sp, sh, sr, kp.buffer_info()[0],
+              None if vp is None else vp.buffer_info()[0], tp, ts)
+    p.pointers = kp, vp   # kept while p is
+    return p
 
 
 def _table(table, n_seq):
@@ -166,9 +172,6 @@ def _table(table, n_seq):
     if se != 1 and width > 1:
         _fail(2, "the table must have contiguous rows")
     return table.data_ptr(), width, ts if n_seq > 1 else width
-
-
-_P1 = _P * 1
 
 
 def _one_layer(k, v, dtype, table, n_seq, d):
@@ -187,7 +190,11 @@ def _one_layer(k, v, dtype, table, n_seq, d):
     if se != 1 and d > 1:
         _fail(2, "the pages must have contiguous elements")
     tp, width, ts = _table(table, n_seq)
-    return Pages(1, pages, rows, hkv, d, width, _code(dtype), 0, sp, sh, sr, _P1(k.data_ptr()), _P1(v.data_ptr()), tp, ts)
+    kv = array.array("Q", (k.data_ptr(), v.data_ptr()))
+    at = kv.buffer_info()[0]
+    p = Pages(1, pages, rows, hkv, d, width, _code(dtype), 0, sp, sh, sr, at, at + 8, tp, ts)
+    p.pointers = kv   # kept while p is
+    return p
 
 
 def _code(dtype):
@@ -345,7 +352,7 @@ def apack_pages_copy(pairs, k_pages, v_pages=(), stream=None):
     pairs: int32 CUDA tensor [n, 2]; k_pages, v_pages: per layer [pages, heads,
     rows, d], or one tensor [layers, pages, heads, rows, d]."""
     first = _first(k_pages, "k_pages")
-    index = _on_device((pairs, first, _first(v_pages, "v_pages") if len(v_pages) else first), "pairs k_pages v_pages")
+    index = _on_device((pairs, first, _first(v_pages, "v_pages") if _given(v_pages) else first), "pairs k_pages v_pages")
     p = _int32(pairs, "pairs", 2)
     if pairs.shape[1] != 2:
         _fail(2, "pairs must be [n, 2]")
@@ -363,8 +370,8 @@ def apack_compact_kv_pages(src_rows, seqs, k_in, v_in, k_out, v_out, table_in=No
     rows, d]; a list of layers or one tensor with layers first."""
     n = len(seqs)
     first = _first(k_in, "k_in")
-    index = _on_device((first, _first(k_out, "k_out"), _first(v_in, "v_in") if len(v_in) else first,
-                        _first(v_out, "v_out") if len(v_out) else first, first if src_rows is None else src_rows,
+    index = _on_device((first, _first(k_out, "k_out"), _first(v_in, "v_in") if _given(v_in) else first,
+                        _first(v_out, "v_out") if _given(v_out) else first, first if src_rows is None else src_rows,
                         first if table_in is None else table_in, first if table_out is None else table_out),
                        "k_in k_out v_in v_out src_rows table_in table_out")
     moves = (Move * max(1, n))(*seqs)
@@ -458,6 +465,8 @@ def apack_paged_attention(q, k_pages, v_pages, table, lens, max_len, mask=None, 
     if workspace is None:
         need = lib.apack_paged_attention_workspace(n, hq, pages.hkv, d, max_len)
         workspace = _new(stream, (max(need, 256),), torch.uint8, q.device)
+    elif not workspace.is_contiguous():
+        _fail(2, "workspace must be contiguous")
     _check(lib.apack_paged_attention(n, hq, qh, _heads(out, "out", dtype), sp, pages, lp, max_len, mp, ms, int(window),
                                      0.0 if scale is None else float(scale), workspace.data_ptr(),
                                      workspace.numel() * workspace.element_size(), _stream_on(stream, index)))

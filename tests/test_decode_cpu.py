@@ -180,9 +180,10 @@ def _pages(n_layers=1, n_pages=4, page_rows=16, hkv=2, d=64, dtype=0, table=FAKE
     p.n_layers, p.n_pages, p.page_rows, p.hkv, p.d, p.dtype = n_layers, n_pages, page_rows, hkv, d, dtype
     p.row_stride, p.head_stride, p.page_stride = d, page_rows * d, hkv * page_rows * d
     n = max(1, min(n_layers, 100))
-    p.k = (ctypes.c_void_p * n)(*[k0 + (i << 28) for i in range(n)])
+    p.pointers = [(ctypes.c_void_p * n)(*[x + (i << 28) for i in range(n)]) for x in (k0, v0)]
+    p.k = ctypes.addressof(p.pointers[0])
     if v:
-        p.v = (ctypes.c_void_p * n)(*[v0 + (i << 28) for i in range(n)])
+        p.v = ctypes.addressof(p.pointers[1])
     p.table, p.table_width, p.table_stride = table, width, width
     for name, x in kw.items():
         setattr(p, name, x)

@@ -901,3 +901,33 @@ def test_binding_refusals():
             log(f"call {i} was not refused")
     torch.cuda.synchronize()
     np.testing.assert_array_equal(bits(kp), bits(k0))
+
+
+def test_layers_as_a_list_and_as_one_tensor():
+    """K a list of layers and V one tensor, and the other way round."""
+    import paper_2608_08794_amd as A
+    g = _gen(59)
+    kv = _rand(g, "bf16", 3, 2, 5, 2, 8, 16)
+    pairs = torch.tensor([[1, 4], [0, 2]], dtype=torch.int32, device="cuda")
+    want = kv.clone()
+    want[:, :, 4], want[:, :, 2] = kv[:, :, 1], kv[:, :, 0]
+    for k_list, v_list in ((True, False), (False, True), (True, True), (False, False)):
+        got = kv.clone()
+        k, v = got[:, 0], got[:, 1]
+        A.apack_pages_copy(pairs, list(k) if k_list else k, list(v) if v_list else v)
+        np.testing.assert_array_equal(bits(got), bits(want))
+    for k, v in ((list(kv[:, 0]), kv[:2, 1]), (kv[:, 0], list(kv[:, 1].float())), (kv[:, 0], kv[:, 1, :, :1])):
+        with pytest.raises(A.ApackError):
+            A.apack_pages_copy(pairs, k, v)
+
+
+def test_workspace_with_gaps_is_refused():
+    import paper_2608_08794_amd as A
+    g = _gen(61)
+    kp, vp, table, n = _paged(g, "bf16", [30, 4], 2, 16, 64)
+    q = _rand(g, "bf16", 4, 2, 64)
+    need = max(256, A.apack_paged_attention_workspace(2, 4, 2, 64, 30))
+    for ws in (torch.empty(1, dtype=torch.uint8, device="cuda").expand(need),
+               torch.empty(2 * need, dtype=torch.uint8, device="cuda")[::2]):
+        with pytest.raises(A.ApackError):
+            A.apack_paged_attention(q, kp, vp, table, n, 30, workspace=ws)
