@@ -594,7 +594,9 @@ size_t apack_paged_attention_workspace(int64_t n_seq, int32_t hq, int32_t hkv, i
  *   o = sum_j p_j v_j,  p = softmax_j(scale q.k_j)
  * over the rows j in [max(0, lens[s] - window), lens[s]) (window 0: all) whose
  * page is in the pool and whose mask is not 0.  Without such a row o is 0 and
- * lse -inf.  Rows that are left out may hold any bits.
+ * lse -inf, as where every logit is -inf.  Rows that are left out may hold any
+ * bits.  Among the others a NaN gives NaN, as does a logit of +inf, and an
+ * infinity in v gives NaN or itself.
  *
  *   q, out  [hq][n_seq][d]; out overlaps neither q nor the pool.
  *   lse     fp32 [hq][n_seq] out (nullable): ln sum_j exp(scale q.k_j), with

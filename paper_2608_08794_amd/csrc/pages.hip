@@ -443,9 +443,9 @@ apack_status apack_compact_kv_pages(int32_t n_seq, const apack_move* seqs, const
   }
   hipStream_t hs = static_cast<hipStream_t>(stream);
   int64_t done = 0;
-  for (int32_t s0 = 0; s0 < n_seq; s0 += kMaxMoves) {
-    a.n_seq = std::min(kMaxMoves, n_seq - s0);
-    a.seq0 = s0;
+  for (int64_t s0 = 0; s0 < n_seq; s0 += kMaxMoves) {
+    a.n_seq = (int32_t)std::min<int64_t>(kMaxMoves, n_seq - s0);
+    a.seq0 = (int32_t)s0;
     a.kept = src_rows ? src_rows + done : nullptr;
     int64_t rows = 0;
     for (int32_t s = 0; s < a.n_seq; ++s) {

@@ -931,3 +931,34 @@ def test_workspace_with_gaps_is_refused():
                torch.empty(2 * need, dtype=torch.uint8, device="cuda")[::2]):
         with pytest.raises(A.ApackError):
             A.apack_paged_attention(q, kp, vp, table, n, 30, workspace=ws)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_paged_attention_of_infinities(dtype):
+    """Logits of -inf weigh nothing, one of +inf gives NaN; an infinite element of V stays in its element."""
+    import paper_2608_08794_amd as A
+    g = _gen(67)
+    kp, vp, table, n = _paged(g, dtype, [100, 700], 2, 16, 64)
+    kp, vp = kp.nan_to_num(0.0), vp.nan_to_num(0.0)
+    q = _rand(g, dtype, 4, 2, 64).abs() + 1
+    row = lambda s, j: (int(table[s, j // 16]), slice(None), j % 16)
+    want, lse = A.apack_paged_attention(q, kp, vp, table, n, 700, return_lse=True)
+    vi = vp.clone()
+    for s, j in ((0, 40), (1, 600)):
+        vi[row(s, j)][:, 7] = float("inf")
+    got = A.apack_paged_attention(q, kp, vi, table, n, 700)
+    assert not torch.isfinite(got[..., 7]).any()
+    rest = [e for e in range(64) if e != 7]
+    np.testing.assert_array_equal(bits(got[..., rest].contiguous()), bits(want[..., rest].contiguous()))
+    ki = kp.clone()
+    for j in range(100):
+        ki[row(0, j)] = float("-inf")
+    got, l = A.apack_paged_attention(q, ki, vp, table, n, 700, return_lse=True)
+    assert not got[:, 0].any() and torch.isneginf(l[:, 0]).all()
+    np.testing.assert_array_equal(bits(got[:, 1].contiguous()), bits(want[:, 1].contiguous()))
+    np.testing.assert_array_equal(bits(l[:, 1].contiguous()), bits(lse[:, 1].contiguous()))
+    ki = kp.clone()
+    ki[row(1, 333)] = float("inf")
+    got = A.apack_paged_attention(q, ki, vp, table, n, 700)
+    assert got[:, 1].isnan().all()
+    np.testing.assert_array_equal(bits(got[:, 0].contiguous()), bits(want[:, 0].contiguous()))
