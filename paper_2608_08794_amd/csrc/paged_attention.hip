@@ -609,16 +609,18 @@ __global__ __launch_bounds__(kThreads) void k_join_parts(const AttnArgs a) {
 }
 
 // Spans that one workgroup takes whole: at most kWholeSpan rows (one sequence of 512
-// rows of 28 heads over 4: 8.4 us, 9.5 in shares and a join), or kWholeSpanMany where
-// the items fill the compute units (64 sequences of 1000 to 2048 rows: 39 us, 42 in
-// shares).  Longer ones of few items would leave most of the chip idle: one sequence
-// of 1024 rows takes 13 us whole, 9 in shares.
-constexpr int64_t kWholeSpan = 512, kWholeSpanMany = 2048, kManyItems = 256;
+// rows of 28 heads over 4: 8.4 us, 9.5 in shares and a join), and more where items are
+// many, kRowsPerItem for each of them (32 sequences, 128 items: of 500 to 1024 rows
+// 18.8 us, 21.4 in shares; to 1400 rows 24.2 either way; to 2048 rows 33.5, 28.8), up to
+// kWholeSpanMany (64 sequences of 1000 to 2048 rows: 39 us, 42 in shares).  Longer ones
+// of few items would leave most of the chip idle: one sequence of 1024 rows takes 13 us
+// whole, 9 in shares.
+constexpr int64_t kWholeSpan = 512, kWholeSpanMany = 2048, kRowsPerItem = 11;
 
 // Shares of k_attend_shares, 0 for one workgroup per sequence and item.
 int64_t plan(int64_t n_seq, int64_t items, int64_t span) {
   const int64_t tiles = std::max<int64_t>(1, (span + kTile - 1) / kTile);
-  if (span <= kWholeSpan || (span <= kWholeSpanMany && n_seq * items >= kManyItems)) return 0;
+  if (span <= std::max(kWholeSpan, std::min(kWholeSpanMany, kRowsPerItem * n_seq * items))) return 0;
   return std::min<int64_t>(kShares, (n_seq * items * tiles + kLeast - 1) / kLeast);
 }
 
