@@ -16,9 +16,10 @@
 // Probabilities, maxima, sums and rescaling of a head all sit in its lane.
 //
 // The rows of all sequences and key heads, in tiles of 32, are dealt to the
-// workgroups in equal shares, whatever the lengths on the device are.  Where a
-// share's border falls inside a sequence's key head, each side leaves its
-// maximum, sum and unnormalised output, and a second kernel joins them.
+// workgroups in equal shares (those of a few sequences key head by key head), whatever
+// the lengths on the device are.  Where a share's border falls inside a sequence's
+// key head, each side leaves its maximum, sum and unnormalised output, and a second
+// kernel joins them.
 //
 // Measured (bf16, 28 heads over 4 of 128, pages of 16 rows), of 6.8 to 7.1 TB/s at
 // which nontemporal loads read this much alone: 64 sequences of 700 to 9454 rows
@@ -45,7 +46,6 @@ constexpr int kWaves = 4;         // of a workgroup
 // loaded ahead take 128 of them); a share is a tile at least: with four, one a wave,
 // four fp32 sequences of up to 1312 rows take 11.6 us, not 8.6.
 constexpr int kShares = 2048 / kWaves;
-constexpr int kLeast = 1;
 template <int D> constexpr int kPart = D + 4;   // floats of a head's part: output, maximum, sum, 16-byte aligned
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
@@ -503,37 +503,81 @@ __device__ __forceinline__ int64_t share_start(int64_t w, int64_t all, int64_t s
   return quotient(w * all, shares);
 }
 
+__device__ __forceinline__ uint32_t of_lane(uint32_t x, int lane) { return (uint32_t)__builtin_amdgcn_readlane(x, lane); }
+
 template <class T, int D, bool kAligned, bool kMask>
 __global__ __launch_bounds__(64 * kWaves, 2) void k_attend_shares(const AttnArgs a) {
   const int items = a.hkv * a.tiles;
   const int share = blockIdx.x;
   __shared__ Joint<D> sh;
 
-  // Tiles of all sequences, and the sequence of this share's first one: each
-  // lane adds up a run of sequences.
+  // Tiles of all sequences: each lane adds up a run of them.
   const int lane = threadIdx.x & 63;
   const int64_t per = (a.n_seq + 63) / 64;
   uint32_t mine = 0;
   for (int64_t i = 0; i < per; ++i)
     if (lane * per + i < a.n_seq) mine += rows_of(a, lane * per + i).tiles;
   const uint32_t upto = sum_upto(mine);
-  const int64_t all = (int64_t)(uint32_t)__builtin_amdgcn_readlane(upto, 63) * items;
-  // No share is smaller than kLeast tiles (as far as there are so many).
-  const int64_t shares = max((int64_t)1, min((int64_t)a.shares, all / kLeast));
-  if (share >= shares) return;
-  const int64_t x0 = share_start(share, all, shares), x1 = share_start(share + 1, all, shares);
-  const int owner = __popcll(__ballot((int64_t)upto * items <= x0));   // the lane whose run holds tile x0
-  int64_t seq = owner * per;
-  int64_t base = (int64_t)(uint32_t)(__builtin_amdgcn_readlane(upto, owner) - __builtin_amdgcn_readlane(mine, owner)) * items;
-  Rows of = rows_of(a, seq);
-  while (x0 >= base + (int64_t)of.tiles * items) {
-    base += (int64_t)of.tiles * items;
-    of = rows_of(a, ++seq);
+  const int64_t all = (int64_t)of_lane(upto, 63) * items;
+  const int64_t shares = min((int64_t)a.shares, all);   // no share is smaller than a tile
+
+  // A border inside a share costs it the chain of first loads once more.  With few
+  // sequences it is spared: each item is dealt in parts of its own, of up to `most`
+  // tiles, as long as that makes a share at most two tiles longer than an equal one
+  // (three sequences of 1000 to 4000 rows 14.1 us, 17.2 in equal shares; ten of 136 to
+  // 1090 13.1, 16.0; sixteen of 1024, whose borders happen to be the shares', lose: 16.3,
+  // 14.5).  One sequence's borders are too few to count (94028 rows 40.9 us, 38.7 in equal
+  // shares), and a tile each leaves none inside.
+  const int64_t pieces = a.n_seq * items;
+  const bool own = a.n_seq > 1 && all > shares && pieces < shares && all * pieces <= 2 * shares * (shares - pieces);
+
+  int64_t seq, base = 0, x0 = 0, x1;
+  int item = 0, t0 = 0, t1 = 0, parts = 0;
+  Rows of;
+  if (own) {
+    const int most = (int)quotient(all - 1, shares - pieces) + 1;   // so that all / most + pieces <= shares
+    auto parts_of = [&](const Rows& r) { return (int)quotient(r.tiles - 1, most) + 1; };
+    uint32_t my_parts = 0;
+    for (int64_t i = 0; i < per; ++i)
+      if (lane * per + i < a.n_seq) my_parts += parts_of(rows_of(a, lane * per + i));
+    const uint32_t parts_upto = sum_upto(my_parts);
+    if (share >= (int64_t)of_lane(parts_upto, 63) * items) return;
+    const int owner = __popcll(__ballot((int64_t)parts_upto * items <= share));   // the lane whose run holds the share
+    int left = share - (int)(of_lane(parts_upto, owner) - of_lane(my_parts, owner)) * items;
+    seq = owner * per;
+    of = rows_of(a, seq);
+    parts = parts_of(of);
+    while (left >= parts * items) {
+      left -= parts * items;
+      of = rows_of(a, ++seq);
+      parts = parts_of(of);
+    }
+    item = (int)quotient(left, parts);
+    const int64_t part = left - item * parts;
+    t0 = (int)quotient(part * of.tiles, parts);
+    t1 = (int)quotient((part + 1) * of.tiles, parts);
+    x1 = t1 - t0;
+  } else {
+    if (share >= shares) return;
+    x0 = share_start(share, all, shares);
+    x1 = share_start(share + 1, all, shares);
+    const int owner = __popcll(__ballot((int64_t)upto * items <= x0));   // the lane whose run holds tile x0
+    base = (int64_t)(of_lane(upto, owner) - of_lane(mine, owner)) * items;
+    seq = owner * per;
+    of = rows_of(a, seq);
+    while (x0 >= base + (int64_t)of.tiles * items) {
+      base += (int64_t)of.tiles * items;
+      of = rows_of(a, ++seq);
+    }
   }
   for (int64_t x = x0; x < x1;) {
-    const int item = (int)quotient(x - base, of.tiles);
-    const int64_t first = base + (int64_t)item * of.tiles;   // the item's first tile
-    const int t0 = (int)(x - first), t1 = (int)min((int64_t)of.tiles, t0 + (x1 - x));
+    int64_t first = 0;             // the item's first tile
+    if (!own) {
+      item = (int)quotient(x - base, of.tiles);
+      first = base + (int64_t)item * of.tiles;
+      t0 = (int)(x - first);
+      t1 = (int)min((int64_t)of.tiles, t0 + (x1 - x));
+    }
     const bool whole = t0 == 0 && t1 == of.tiles;
     const int slot = 2 * share + (x == x0 ? 0 : 1);
     Wave<T, D, kAligned, kMask> w(a, seq, of, item);
@@ -541,10 +585,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_attend_shares(const AttnArgs
     if (x > x0) __syncthreads();   // the item before has been read from LDS
     sh.join(w, static_cast<T*>(a.out), whole ? nullptr : a.part + (int64_t)slot * min(kHeads, a.group) * kPart<D>);
     if (threadIdx.x == 0 && t0 == 0) {
-      // The item's last share is the last one that starts before its end.
-      const int64_t last = whole ? 0 : quotient((first + of.tiles) * shares - 1, all);
+      // An item's last equal share is the last one that starts before its end.
+      if (!own) parts = whole ? 1 : (int)(quotient((first + of.tiles) * shares - 1, all) - share) + 1;
       int32_t* to = a.split + 3 * (seq * items + item);
-      to[0] = whole ? 0 : (int32_t)(last - share) + 1;
+      to[0] = whole ? 0 : parts;
       to[1] = slot;
       to[2] = share;
     }
@@ -621,7 +665,7 @@ constexpr int64_t kWholeSpan = 512, kWholeSpanMany = 2048, kRowsPerItem = 11;
 int64_t plan(int64_t n_seq, int64_t items, int64_t span) {
   const int64_t tiles = std::max<int64_t>(1, (span + kTile - 1) / kTile);
   if (span <= std::max(kWholeSpan, std::min(kWholeSpanMany, kRowsPerItem * n_seq * items))) return 0;
-  return std::min<int64_t>(kShares, (n_seq * items * tiles + kLeast - 1) / kLeast);
+  return std::min<int64_t>(kShares, n_seq * items * tiles);
 }
 
 // Row numbers, up to a few thousand past max_len where steps are looked ahead, are 32-bit; tiles of all sequences

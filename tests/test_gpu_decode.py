@@ -962,3 +962,21 @@ def test_paged_attention_of_infinities(dtype):
     got = A.apack_paged_attention(q, ki, vp, table, n, 700)
     assert got[:, 1].isnan().all()
     np.testing.assert_array_equal(bits(got[:, 0].contiguous()), bits(want[:, 0].contiguous()))
+
+
+@pytest.mark.parametrize("dtype,hkv,lens,window", [
+    ("bf16", 1, [0, 1, 5000, 31, 33, 0, 2500] * 10, 0),
+    ("bf16", 4, [900, 0, 4001], 0),
+    ("f32", 2, [3000, 2999, 1, 640, 0, 17], 0),
+    ("bf16", 2, [5000, 4000, 700, 3, 0], 2049),
+    ("f32", 8, [700, 513], 0)])
+def test_paged_attention_of_few_ragged_sequences(dtype, hkv, lens, window):
+    """Long spans of few sequences: every key head of a sequence is split on its own."""
+    import paper_2608_08794_amd as A
+    g = _gen(71)
+    kp, vp, table, n = _paged(g, dtype, lens, hkv, 16, 128)
+    q = _rand(g, dtype, 2 * hkv, len(lens), 128)
+    o, lse = A.apack_paged_attention(q, kp, vp, table, n, 5000, window=window, return_lse=True)
+    _check_attention(o, lse, q, kp, vp, table, n, 5000, window=window, dtype=dtype)
+    again = A.apack_paged_attention(q, kp, vp, table, n, 5000, window=window)
+    np.testing.assert_array_equal(bits(again), bits(o))
