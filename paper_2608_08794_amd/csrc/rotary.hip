@@ -86,6 +86,27 @@ __device__ __forceinline__ void turn_pair(float a, float b, float c, float s, T*
   from_f(__builtin_fmaf(a, s, b * c), y);
 }
 
+// Sine and cosine of x turns, |x| <= 1/2: an eighth of a turn or less from a whole
+// quarter, where the Taylor series to the 9th and 10th power are off by less than 2^-28.
+// Half as long as the library's, which takes any angle: 12998 rows of 18 heads of 64
+// take 16.0 us, 17.2 with it, one row's append 3.9, 4.2.
+__device__ __forceinline__ void sincos_turns(float x, float* s, float* c) {
+  const float q = __builtin_rintf(4.0f * x), r = __builtin_fmaf(q, -0.25f, x), t = r * r;
+  float a = __builtin_fmaf(t, 4.205869394e+01f, -7.670585975e+01f);
+  a = __builtin_fmaf(t, a, 8.160524928e+01f);
+  a = __builtin_fmaf(t, a, -4.134170224e+01f);
+  a = r * __builtin_fmaf(t, a, 6.283185307e+00f);
+  float b = __builtin_fmaf(t, -2.642625678e+01f, 6.024464137e+01f);
+  b = __builtin_fmaf(t, b, -8.545681721e+01f);
+  b = __builtin_fmaf(t, b, 6.493939402e+01f);
+  b = __builtin_fmaf(t, b, -1.973920880e+01f);
+  b = __builtin_fmaf(t, b, 1.0f);
+  const int n = (int)q;                     // quarters: -2 to 2
+  const uint32_t sn = __float_as_uint(n & 1 ? b : a), cn = __float_as_uint(n & 1 ? a : b);
+  *s = __uint_as_float(sn ^ ((uint32_t)n & 2) << 30);
+  *c = __uint_as_float(cn ^ ((uint32_t)(n + 1) & 2) << 30);
+}
+
 // T: uint16_t (bf16 bits) or float.  A thread has VEC elements from e0 and VEC from
 // e1 on, half of what turns (or of what does not) apart, so that the lanes of either
 // load lie side by side.  The VEC pairs are (e0 + j, e1 + j) (kHalf), or two by two
@@ -113,8 +134,8 @@ __global__ __launch_bounds__(kThreads) void k_rotary(const RotaryArgs a) {
   const bool second = e1 < a.d;  // an odd d ends in a single element
 
   // Vectors: the positions are asked for first, the rows' elements next, and the
-  // angles come while those are on their way (256 sequences' append 4.7 us, 5.6 with
-  // the angles first).  Single elements, many heads a thread, have them before.
+  // angles come while those are on their way (which takes 0.9 us off 256 sequences'
+  // append).  Single elements, many heads a thread, have them before.
   int32_t p[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) p[j] = turned && j < a.pos_rows ? a.pos[j * a.pos_stride + row] : 0;
@@ -130,7 +151,7 @@ __global__ __launch_bounds__(kThreads) void k_rotary(const RotaryArgs a) {
       // less than 2^-24 turns, where an fp32 angle would be off by whole turns.
       const double x = __builtin_rint((double)at * a.turns[i]);
       float s, k;
-      sincospif(2.0f * (float)__builtin_fma((double)at, a.turns[i], -x), &s, &k);
+      sincos_turns((float)__builtin_fma((double)at, a.turns[i], -x), &s, &k);
       cs[j] = k * a.factor;
       sn[j] = s * a.factor * a.sign;
     }
