@@ -10,6 +10,9 @@ from ._lib import ApackError, _alloc_on, _check, _torch, library
 ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
 ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "by_parts": 3}
 
+# Address of a table without entries, which torch gives none: never read, and not NULL, which stands for planes.
+_NO_ENTRIES = 256
+
 _P = ctypes.c_void_p
 _I32, _I64, _SZ, _F64 = ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t, ctypes.c_double
 
@@ -171,7 +174,7 @@ def _table(table, n_seq):
     ts, se = table.stride()
     if se != 1 and width > 1:
         _fail(2, "the table must have contiguous rows")
-    return table.data_ptr(), width, ts if n_seq > 1 else width
+    return table.data_ptr() or _NO_ENTRIES, width, ts if n_seq > 1 else width
 
 
 def _one_layer(k, v, dtype, table, n_seq, d):

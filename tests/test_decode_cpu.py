@@ -401,3 +401,22 @@ def test_binding_refuses_host_tensors():
             call()
     with pytest.raises(A.ApackError):
         A.apack_rotary(i, rope)
+
+
+# -- tables, masks and position ids at their edges ----------------------------
+
+def _compact_of(pin, pout, seqs):
+    return _status("apack_compact_kv_pages", len(seqs), (D.Move * len(seqs))(*seqs), None, pin, pout, None)
+
+
+def test_table_without_entries_is_a_table():
+    """torch gives a tensor of no elements no address, and a NULL table says that the tensors are planes."""
+    x, y = (torch.zeros(1, 2, 16, 64) for _ in range(2))
+    empty = torch.empty(1, 0, dtype=torch.int32)
+    pages = D._pages([y], [], empty, 1)
+    assert pages.table and pages.table_width == 0
+    st, msg = _compact_of(D._pages([x[0]], [], planes=True), pages, [(0, 16, 0, 4)])
+    assert st == 2 and "past the output table" in msg
+    pages = D._one_layer(x, y, x.dtype, torch.zeros(3, 5, dtype=torch.int32)[:, 2:2], 3, 64)
+    assert pages.table and pages.table_width == 0
+    assert not D._pages([y[0]], [], planes=True).table

@@ -980,3 +980,32 @@ def test_paged_attention_of_few_ragged_sequences(dtype, hkv, lens, window):
     _check_attention(o, lse, q, kp, vp, table, n, 5000, window=window, dtype=dtype)
     again = A.apack_paged_attention(q, kp, vp, table, n, 5000, window=window)
     np.testing.assert_array_equal(bits(again), bits(o))
+
+
+# ---------------------------------------------------------------------------
+# Tables, masks and position ids at their edges
+# ---------------------------------------------------------------------------
+
+def test_tables_without_entries():
+    """Every row is beyond such a table, also where the pool is one page."""
+    import paper_2608_08794_amd as A
+    g = _gen(81)
+    kp, vp = (_rand(g, "bf16", 1, 2, 16, 64) for _ in range(2))
+    k0, v0 = kp.clone(), vp.clone()
+    q, k, v = (_rand(g, "bf16", h, 3, 64) for h in (4, 2, 2))
+    n = torch.tensor([1, 5, 16], dtype=torch.int32, device="cuda")
+    rope = A.apack_rope(64)
+    for table in (torch.empty(3, 0, dtype=torch.int32, device="cuda"),
+                  torch.zeros(3, 4, dtype=torch.int32, device="cuda")[:, 2:2]):
+        o, lse = A.apack_paged_attention(q, kp, vp, table, n, 16, return_lse=True)
+        assert not o.any() and torch.isneginf(lse).all()
+        o, lse = A.apack_paged_attention(q, kp, vp, table, n, 5000, return_lse=True)
+        assert not o.any() and torch.isneginf(lse).all()
+        qt = A.apack_rotary_append(n, rope, q, k, v, kp, vp, table, n)
+        assert torch.equal(qt, A.apack_rotary(n, rope, q)[0])
+        plane = torch.full((2, 16, 64), 7.0, dtype=torch.bfloat16, device="cuda")
+        A.apack_compact_kv_pages(None, [(0, 16, 0, 16), (0, 0, 0, 0), (0, 0, 0, 0)], [kp], [], [plane], [], table_in=table)
+        assert (plane == 7).all()
+        with pytest.raises(A.ApackError, match="past the output table"):
+            A.apack_compact_kv_pages(None, [(0, 16, 0, 1)] + [(0, 0, 0, 0)] * 2, [plane], [], [kp], [], table_out=table)
+        assert torch.equal(kp, k0) and torch.equal(vp, v0)
