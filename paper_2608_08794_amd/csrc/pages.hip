@@ -410,13 +410,16 @@ apack_status apack_compact_kv_pages(int32_t n_seq, const apack_move* seqs, const
   const Strided t_in = rows_of_stride(in->table, 4, n_seq, in->table_stride, in->table_width);
   const Strided t_out = rows_of_stride(out->table, 4, n_seq, out->table_stride, out->table_width);
   APACK_CHECK(t_in.ok && t_out.ok, APACK_E_SHAPE, "a table of 2^46 entries or more");
+  Strided o = tout, other_in = tin, other_out = tout;
   for (size_t i = 0; i < outs.size(); ++i) {
-    const Strided o = at(tout, outs[i]);
+    o.data = outs[i];
     APACK_CHECK(apart(o, kept) && apart(o, t_in) && apart(o, t_out), APACK_E_ALIAS,
                 "an output overlaps src_rows or a table");
     for (size_t j = 0; j < ins.size(); ++j) {
-      APACK_CHECK((one && i == j) || apart(o, at(tin, ins[j])), APACK_E_ALIAS, "an output overlaps an input");
-      APACK_CHECK(j <= i || apart(o, at(tout, outs[j])), APACK_E_ALIAS, "two outputs overlap");
+      other_in.data = ins[j];
+      other_out.data = outs[j];
+      APACK_CHECK((one && i == j) || apart(o, other_in), APACK_E_ALIAS, "an output overlaps an input");
+      APACK_CHECK(j <= i || apart(o, other_out), APACK_E_ALIAS, "two outputs overlap");
     }
   }
   if (total == 0) return APACK_OK;

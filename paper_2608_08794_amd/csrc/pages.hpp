@@ -34,14 +34,15 @@ struct FastDiv {
 
 // The elements of a tensor of up to three strided dimensions over contiguous
 // runs: `ok` when all of them are distinct, `extent` elements from the first
-// to the last, and the outermost dimension's stride and what lies within one
-// step of it.
+// to the last, and the dimensions of more than one step as (stride, steps), the
+// innermost first: a stride is no shorter than what lies within it.
 struct Strided {
   const void* data = nullptr;
   size_t es = 2;
   bool ok = true;
-  int64_t extent = 0, outer_stride = 0, inner = 0;
-  int n = 0;                 // dimensions of more than one step
+  int64_t extent = 0, run = 0;
+  std::pair<int64_t, int64_t> dim[3];
+  int n = 0;
 };
 
 // run: contiguous elements; (stride, count) pairs in any order.
@@ -50,17 +51,14 @@ inline Strided strided(const void* data, size_t es, int64_t run,
   Strided t;
   t.data = data;
   t.es = es;
-  t.inner = run;
-  std::pair<int64_t, int64_t> by[3];
+  t.run = run;
   for (auto& dim : dims)
-    if (dim.second > 1) by[t.n++] = dim;
-  std::sort(by, by + t.n);
+    if (dim.second > 1) t.dim[t.n++] = dim;
+  std::sort(t.dim, t.dim + t.n);
   __int128 at = run;
   for (int i = 0; i < t.n; ++i) {
-    t.ok &= by[i].first >= at;
-    t.inner = (int64_t)at;
-    t.outer_stride = by[i].first;
-    at += (__int128)by[i].first * (by[i].second - 1);
+    t.ok &= t.dim[i].first >= at;
+    at += (__int128)t.dim[i].first * (t.dim[i].second - 1);
     t.ok &= at >= 0 && at <= (__int128(1) << 46);
     if (!t.ok) return t;
   }
@@ -68,17 +66,30 @@ inline Strided strided(const void* data, size_t es, int64_t run,
   return t;
 }
 
-// Whether no element of a is one of b: their byte ranges are apart, or they
-// interleave (equal strides, as slices of one tensor, each within its part of
-// the outermost step).
+// Whether the elements of a's la inner dimensions are none of those of b's lb inner
+// ones, ea and eb elements long, with b's first `at` elements after a's: their ranges
+// are apart, or they interleave at equal strides S.  Two elements of steps i and j of
+// S then meet only where i S + x = at + j S + y; x and y lie in [0, S), so with
+// at = q S + m, 0 <= m < S, either i - j = q and x = y + m, or i - j = q + 1 and
+// x = y + m - S.
+inline bool apart_at(const Strided& a, int la, int64_t ea, const Strided& b, int lb, int64_t eb, int64_t at) {
+  if (at >= ea || at + eb <= 0) return true;
+  if (!la || !lb || a.dim[la - 1].first != b.dim[lb - 1].first) return false;
+  const int64_t stride = a.dim[la - 1].first, i = a.dim[la - 1].second - 1, j = b.dim[lb - 1].second - 1;
+  const int64_t q = at / stride - (at % stride < 0), m = at - q * stride;
+  ea -= stride * i;
+  eb -= stride * j;
+  return (q < -j || q > i || apart_at(a, la - 1, ea, b, lb - 1, eb, m)) &&
+         (q + 1 < -j || q + 1 > i || apart_at(a, la - 1, ea, b, lb - 1, eb, m - stride));
+}
+
+// Whether no element of a is one of b: their byte ranges are apart, or they interleave
+// at equal strides (slices of one tensor, of any of its dimensions).
 inline bool apart(const Strided& a, const Strided& b) {
   if (!overlaps(a.data, (size_t)a.extent * a.es, b.data, (size_t)b.extent * b.es)) return true;
-  if (a.es != b.es || !a.n || !b.n || a.outer_stride != b.outer_stride) return false;
   const int64_t bytes = (int64_t)((uintptr_t)b.data - (uintptr_t)a.data);
-  if (bytes % (int64_t)a.es) return false;
-  int64_t at = bytes / (int64_t)a.es % a.outer_stride;
-  if (at < 0) at += a.outer_stride;
-  return at >= a.inner && a.outer_stride - at >= b.inner;
+  if (a.es != b.es || bytes % (int64_t)a.es) return false;
+  return apart_at(a, a.n, a.extent, b, b.n, b.extent, bytes / (int64_t)a.es);
 }
 
 // A contiguous range as a Strided.

@@ -420,3 +420,56 @@ def test_table_without_entries_is_a_table():
     pages = D._one_layer(x, y, x.dtype, torch.zeros(3, 5, dtype=torch.int32)[:, 2:2], 3, 64)
     assert pages.table and pages.table_width == 0
     assert not D._pages([y[0]], [], planes=True).table
+
+
+def _elements(k0, p):
+    return {k0 // 2 + i * p.page_stride + h * p.head_stride + r * p.row_stride + e
+            for i in range(p.n_pages) for h in range(p.hkv) for r in range(p.page_rows) for e in range(p.d)}
+
+
+def test_overlap_is_found_and_slices_of_one_tensor_pass():
+    """Pools of one to three dimensions at small strides: any element in common is an alias; slices of one dimension of
+    a larger tensor are none.  Nothing is moved."""
+    rng = np.random.default_rng(7)
+    met = passed = 0
+    for turn in range(4000):
+        d, counts = int(rng.integers(1, 4)), rng.integers(1, 4, 3)
+        order = rng.permutation(3)
+        # A larger tensor of which both sides are slices: `extra` times as many of one dimension, or of the run.
+        extra, where = int(rng.integers(1, 4)), int(rng.integers(0, 4))
+        strides, at = np.zeros(3, dtype=int), d * (extra if where == 3 else 1)
+        for i in order:
+            strides[i] = at * (extra if where == i and rng.integers(0, 2) else 1) + int(rng.integers(0, 2))
+            at = strides[i] * counts[i]
+        kw = dict(n_pages=int(counts[0]), hkv=int(counts[1]), page_rows=int(counts[2]), d=d, v=False,
+                  page_stride=int(strides[0]), head_stride=int(strides[1]), row_stride=int(strides[2]))
+        shift = 2 * int(rng.integers(1, max(2, at + 2)))
+        pin, pout = _pages(k0=FAKE, **kw), _pages(k0=FAKE + shift, **kw)
+        if turn % 3 == 0:                                    # other counts at the same strides
+            kw["page_rows"] = 1
+            pout = _pages(k0=FAKE + shift, **kw)
+        st, _ = _compact([(0, 1, 0, 0)], src=None, pin=pin, pout=pout)
+        if _elements(FAKE, pin) & _elements(FAKE + shift, pout):
+            assert st == 5, (kw, shift)
+            met += 1
+        else:
+            passed += st == 0
+            assert st == 0 or turn % 3 == 0, (kw, shift)     # all three strides alike: exact
+    assert met > 500 and passed > 500
+
+
+def test_slices_within_the_heads_are_apart():
+    # [pages][heads][K and V][rows][d].
+    kw = dict(hkv=4, head_stride=2 * 16 * 64, page_stride=4 * 2 * 16 * 64)
+    pin = _pages(v0=FAKE + 16 * 64 * 2, **kw)
+    pout = _pages(k0=FAKE + (3 << 34), v0=FAKE + (3 << 34) + 16 * 64 * 2, **kw)
+    assert _compact([(0, 4, 0, 0)], pin=pin, pout=pout)[0] == 0
+    pout = _pages(k0=FAKE + (3 << 34), v0=FAKE + (3 << 34) + 16 * 64, **kw)      # half the rows over
+    assert _compact([(0, 4, 0, 0)], pin=pin, pout=pout)[0] == 5
+    # A projection [rows][heads][q, k and v][d], turned in place: refused only further on, for its many rows.
+    rows, d, far = 1 << 25, 511, FAKE << 12
+    q, k = (_heads(far + 2 * i * d, 2, rows, d, head_stride=3 * d, row_stride=6 * d) for i in range(2))
+    st, msg = _rotary(rows=rows, stride=rows, d=d, pos=FAKE, q=q, qo=q, k=k, ko=k)
+    assert st == 7 and "too many rows" in msg
+    k = _heads(far + d, 2, rows, d, head_stride=3 * d, row_stride=6 * d)
+    assert _rotary(rows=rows, stride=rows, d=d, pos=FAKE, q=q, qo=q, k=k, ko=k)[0] == 5

@@ -1009,3 +1009,39 @@ def test_tables_without_entries():
         with pytest.raises(A.ApackError, match="past the output table"):
             A.apack_compact_kv_pages(None, [(0, 16, 0, 1)] + [(0, 0, 0, 0)] * 2, [plane], [], [kp], [], table_out=table)
         assert torch.equal(kp, k0) and torch.equal(vp, v0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_slices_within_the_heads(dtype):
+    """A projection [rows][heads][q, k and v][d] turned in place, and pools [pages][heads][K and V][rows][d]."""
+    import paper_2608_08794_amd as A
+    g = _gen(82)
+    rope = _rope(64)
+    fused = _rand(g, dtype, 40, 2, 3, 64)
+    q, k, v = (x.transpose(0, 1) for x in fused.unbind(2))
+    pos = torch.randint(0, 9000, (40,), generator=g, device="cuda", dtype=torch.int32)
+    v0 = v.clone()
+    qw, kw = A.apack_rotary(pos, rope, q.contiguous(), k.contiguous())
+    A.apack_rotary(pos, rope, q, k, q_out=q, k_out=k)
+    assert torch.equal(q, qw) and torch.equal(k, kw) and torch.equal(v, v0)
+    pool, other = (_rand(g, dtype, 6, 2, 2, 16, 64) for _ in range(2))
+    (kp, vp), (ko, vo) = pool.unbind(2), other.unbind(2)
+    k1, v1 = kp.clone(), vp.clone()
+    table = torch.tensor([[4, 1, 5]], dtype=torch.int32, device="cuda")
+    A.apack_compact_kv_pages(None, [(0, 40, 0, 40)], [k], [v], [kp], [vp], table_out=table)
+    for j in range(40):
+        page, row = int(table[0, j // 16]), j % 16
+        k1[page, :, row], v1[page, :, row] = k[:, j], v[:, j]
+    assert torch.equal(kp, k1) and torch.equal(vp, v1)
+    n = torch.tensor([41], dtype=torch.int32, device="cuda")
+    new = _rand(g, dtype, 1, 2, 3, 64)
+    q, k, v = (x.transpose(0, 1) for x in new.unbind(2))
+    qt = A.apack_rotary_append(n, rope, q, k, v, kp, vp, table, n, q_out=q)
+    k1[5, :, 8], v1[5, :, 8] = A.apack_rotary(n, rope, k=k)[1][:, 0], v[:, 0]
+    assert torch.equal(kp, k1) and torch.equal(vp, v1)
+    o, lse = A.apack_paged_attention(qt, kp, vp, table, n, 48, return_lse=True)
+    _check_attention(o, lse, qt, kp, vp, table, n, 48, dtype=dtype)
+    table_out = torch.tensor([[2, 0, 3]], dtype=torch.int32, device="cuda")
+    A.apack_compact_kv_pages(None, [(0, 41, 0, 41)], [kp], [vp], [ko], [vo], table_in=table, table_out=table_out)
+    A.apack_pages_copy(torch.tensor([[2, 4], [0, 1], [3, 5]], dtype=torch.int32, device="cuda"), [ko], [vo])
+    assert torch.equal(ko[[4, 1]], k1[[4, 1]]) and torch.equal(vo[5, :, :9], v1[5, :, :9])
