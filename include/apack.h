@@ -584,8 +584,8 @@ apack_status apack_rotary_append(const apack_rope* rope, int64_t n_seq, const in
                                  const apack_heads* q_out, const apack_heads* k,
                                  const apack_heads* v, const apack_pages* pages, void* stream);
 
-/* Workspace bytes of apack_paged_attention for these sizes (0 for sizes that
- * it refuses). */
+/* Workspace bytes of apack_paged_attention for these sizes and for calls of
+ * fewer sequences, a smaller max_len or a window (0 for sizes that it refuses). */
 size_t apack_paged_attention_workspace(int64_t n_seq, int32_t hq, int32_t hkv, int32_t d,
                                        int64_t max_len);
 

@@ -731,7 +731,11 @@ size_t apack_paged_attention_workspace(int64_t n_seq, int32_t hq, int32_t hkv, i
   if (!sizes_ok(n_seq, hq, hkv, d, max_len)) return 0;
   const int group = hq / hkv;
   const int64_t items = (int64_t)hkv * ((group + kHeads - 1) / kHeads);
-  return std::max<size_t>(kAlign, layout(nullptr, plan(n_seq, items, max_len), n_seq, items, group, d).bytes);
+  // The largest need up to these sizes: where so many sequences are taken whole, the most
+  // that are dealt in shares.
+  int64_t n = n_seq;
+  if (plan(n, items, max_len) == 0) n = max_len > kWholeSpan ? std::min(n, (max_len - 1) / (kRowsPerItem * items)) : 0;
+  return std::max<size_t>(kAlign, layout(nullptr, plan(n, items, max_len), n, items, group, d).bytes);
 }
 
 apack_status apack_paged_attention(int64_t n_seq, int32_t hq, const apack_heads* q, const apack_heads* out, float* lse,

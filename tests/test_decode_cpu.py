@@ -473,3 +473,19 @@ def test_slices_within_the_heads_are_apart():
     assert st == 7 and "too many rows" in msg
     k = _heads(far + d, 2, rows, d, head_stride=3 * d, row_stride=6 * d)
     assert _rotary(rows=rows, stride=rows, d=d, pos=FAKE, q=q, qo=q, k=k, ko=k)[0] == 5
+
+
+@pytest.mark.parametrize("hq,hkv", [(28, 4), (4, 2), (8, 8), (32, 1), (16, 16)])
+def test_attention_workspace_covers_smaller_batches(hq, hkv):
+    """A batch that shrinks, as sequences end, decodes on with the workspace of the whole."""
+    f = A.apack_paged_attention_workspace
+    heads = dict(hq=hq, q=_heads(FAKE + (12 << 34), hq, 64, 64), out=_heads(FAKE + (13 << 34), hq, 64, 64))
+    for longest in (0, 1, 512, 513, 700, 1290, 1408, 2047, 2048, 2049, 9454):
+        sizes = [f(n, hq, hkv, 64, longest) for n in range(0, 65)]
+        assert sizes == sorted(sizes)
+        for n in (1, 2, 3, 7, 16, 40, 64):
+            for shorter in (longest, longest // 2, 513):
+                # Refused for its outputs, which are looked at after the workspace.
+                st, _ = _attend(n=n, pages=_pages(hkv=hkv), max_len=min(longest, shorter), lse=FAKE + 64,
+                                ws_bytes=sizes[64], **heads)
+                assert st == 5
