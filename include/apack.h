@@ -459,7 +459,8 @@ typedef struct apack_heads {
  * turn before the sine and cosine, so far positions lose nothing; products and
  * sums are fp32, rounded once.
  *
- *   pos   DEVICE int32 [pos_rows][rows], row stride pos_stride; any value.
+ *   pos   DEVICE int32 [pos_rows][rows], row stride pos_stride (0: the same
+ *         ids in every row); any value.
  *   q_in/q_out, k_in/k_out: either pair may be NULL; heads and strides as
  *   given, d <= 512, rot_dim <= d.  An output may be its own input (the same
  *   data and strides); otherwise it overlaps no input, no other output and not

@@ -276,7 +276,7 @@ def apack_rope(rot_dim, base=10000.0, layout="half", scaling="none", factor=1.0,
 def apack_rotary(pos, rope, q=None, k=None, q_out=None, k_out=None, transpose=None, stream=None):
     """Turns q and k [heads, rows, d] (any order of heads and rows, so a
     transposed [rows, heads, d] projection too) by their position ids pos
-    [pos_rows, rows] int32.  q_out and k_out may be q and k; without them, new
+    [pos_rows, rows] int32 (which may be one row, expanded).  q_out and k_out may be q and k; without them, new
     [heads, rows, d] tensors.  transpose (rope's by default) turns the other
     way: the gradient of the call, and with factor 1 its inverse.  Returns
     (q_out, k_out)."""

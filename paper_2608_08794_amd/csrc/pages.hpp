@@ -95,9 +95,10 @@ inline bool apart(const Strided& a, const Strided& b) {
 // A contiguous range as a Strided.
 inline Strided range(const void* data, size_t bytes) { return strided(data, 1, (int64_t)bytes, {}); }
 
-// `rows` rows of `width` elements at a stride (host checks of tables, masks, position ids).
+// `rows` rows of `width` elements at a stride, one row at a stride of 0 (host checks of
+// tables, masks, position ids).
 inline Strided rows_of_stride(const void* data, size_t es, int64_t rows, int64_t stride, int64_t width) {
-  return data && rows ? strided(data, es, width, {{stride, rows}}) : range(data, 0);
+  return data && rows ? strided(data, es, width, {{stride, stride ? rows : 1}}) : range(data, 0);
 }
 
 // Addressing of a pool (one page that holds the packed rows without a table).

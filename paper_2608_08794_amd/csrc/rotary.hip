@@ -386,7 +386,8 @@ apack_status apack_rotary(const apack_rope* rope, int64_t rows, const int32_t* p
   APACK_CHECK(rows >= 0, APACK_E_SHAPE, "rows must be >= 0");
   APACK_CHECK(rows < (int64_t(1) << 31), APACK_E_UNSUPPORTED, "rows must be < 2^31");
   APACK_CHECK(rows == 0 || pos, APACK_E_ARG, "pos is NULL");
-  APACK_CHECK(rope->pos_rows == 1 || pos_stride >= rows, APACK_E_SHAPE, "pos_stride must be >= rows");
+  APACK_CHECK(rope->pos_rows == 1 || pos_stride >= rows || pos_stride == 0, APACK_E_SHAPE,
+              "pos_stride must be >= rows, or 0");
   APACK_CHECK(!q_in == !q_out && !k_in == !k_out, APACK_E_ARG, "an input without its output, or the reverse");
   const size_t es = dtype_size(dtype);
   Strided ins[2], outs[2];
@@ -435,7 +436,8 @@ apack_status apack_rotary_append(const apack_rope* rope, int64_t n_seq, const in
   APACK_CHECK(n_seq >= 0, APACK_E_SHAPE, "n_seq must be >= 0");
   APACK_CHECK(n_seq < (int64_t(1) << 31), APACK_E_UNSUPPORTED, "n_seq must be < 2^31");
   APACK_CHECK(n_seq == 0 || (pos && lens), APACK_E_ARG, "pos or lens is NULL");
-  APACK_CHECK(rope->pos_rows == 1 || pos_stride >= n_seq, APACK_E_SHAPE, "pos_stride must be >= n_seq");
+  APACK_CHECK(rope->pos_rows == 1 || pos_stride >= n_seq || pos_stride == 0, APACK_E_SHAPE,
+              "pos_stride must be >= n_seq, or 0");
   const size_t es = dtype_size(pages->dtype);
   Strided ins[3], qo;
   const apack_heads* const in[3] = {q_in, k, v};

@@ -489,3 +489,16 @@ def test_attention_workspace_covers_smaller_batches(hq, hkv):
                 st, _ = _attend(n=n, pages=_pages(hkv=hkv), max_len=min(longest, shorter), lse=FAKE + 64,
                                 ws_bytes=sizes[64], **heads)
                 assert st == 5
+
+
+def test_one_row_of_position_ids_for_all():
+    # A row stride of 0; refused further on, q_out lying on its input (q's and lens' overlap for the append).
+    rope = _rope(pos_rows=3, sections=(ctypes.c_int32 * 4)(16, 8, 8, 0))
+    assert _rotary(rope=rope, stride=0, qo=_heads(FAKE + 128, 4, 8, 64))[0] == 5
+    args = [_heads(FAKE + (i << 34), h, 3, 64) for i, h in ((12, 4), (11, 4), (14, 2), (15, 2))]
+    assert _status("apack_rotary_append", rope, 3, FAKE + (10 << 34), 0, FAKE + (11 << 34), *args, _pages(), None)[0] == 5
+    for stride in (1, 7, -8):
+        assert _rotary(rope=rope, stride=stride)[0] == 2
+    # Onto the last of the ids.
+    far = _heads(FAKE + (5 << 34) + 4 * 8, 4, 8, 64)
+    assert _rotary(rope=rope, stride=0, q=far, qo=_heads(FAKE + (5 << 34) + 4 * 7, 4, 8, 64))[0] == 5

@@ -1045,3 +1045,20 @@ def test_slices_within_the_heads(dtype):
     A.apack_compact_kv_pages(None, [(0, 41, 0, 41)], [kp], [vp], [ko], [vo], table_in=table, table_out=table_out)
     A.apack_pages_copy(torch.tensor([[2, 4], [0, 1], [3, 5]], dtype=torch.int32, device="cuda"), [ko], [vo])
     assert torch.equal(ko[[4, 1]], k1[[4, 1]]) and torch.equal(vo[5, :, :9], v1[5, :, :9])
+
+
+@pytest.mark.parametrize("rows", [1, 37])
+def test_position_ids_expanded_from_one_row(rows):
+    """Text tokens have the same id in every row."""
+    import paper_2608_08794_amd as A
+    g = _gen(83)
+    rope = _rope(64, sections=(16, 8, 8))
+    pos = torch.randint(0, 9000, (1, rows), generator=g, device="cuda", dtype=torch.int32).expand(3, rows)
+    q, k, v = (_rand(g, "bf16", h, rows, 64) for h in (4, 2, 2))
+    qt, kt = A.apack_rotary(pos, rope, q, k)
+    _check_turned(qt, q, pos, rope, "half", "bf16")
+    assert torch.equal(kt, A.apack_rotary(pos.contiguous(), rope, k=k)[1])
+    kp, vp = (torch.zeros(rows, 2, 16, 64, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    table = torch.arange(rows, dtype=torch.int32, device="cuda")[:, None]
+    assert torch.equal(A.apack_rotary_append(pos, rope, q, k, v, kp, vp, table, torch.full_like(pos[0], 4)), qt)
+    assert torch.equal(kp[:, :, 3], kt.transpose(0, 1)) and torch.equal(vp[:, :, 3], v.transpose(0, 1))
