@@ -607,7 +607,8 @@ size_t apack_paged_attention_workspace(int64_t n_seq, int32_t hq, int32_t hkv, i
  *   lens    DEVICE int32 [n_seq]; rows beyond max_len or the table are left
  *           out, so max_len (HOST) bounds the lengths that the call can meet:
  *           a captured call may be replayed while lens grow up to it.
- *   mask    DEVICE uint8 [n_seq][max_len] (nullable), row stride mask_stride.
+ *   mask    DEVICE uint8 [n_seq][max_len] (nullable), row stride mask_stride
+ *           (0: the same mask for every sequence).
  *   scale   in [1e-30, 1e30], or 0 for 1/sqrt(d).
  *
  * Several new tokens of one sequence are passed as sequences with equal table

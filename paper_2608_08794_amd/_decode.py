@@ -426,9 +426,10 @@ def apack_paged_attention(q, k_pages, v_pages, table, lens, max_len, mask=None, 
     """Attention of one query row per sequence, q [hq, n_seq, d], over its rows
     of one layer's paged cache ([pages, hkv, rows, d] tensors, table [n_seq,
     pages] int32, lens [n_seq] int32 of at most max_len rows).  mask: bool or
-    uint8 [n_seq, max_len], rows to attend to; window: only the last so many
-    rows (0: all); scale: 1/sqrt(d) by default.  Returns out [hq, n_seq, d] (new
-    if not given), and with return_lse (out, lse [hq, n_seq] fp32)."""
+    uint8 [n_seq, max_len] (which may be one row, expanded), rows to attend to;
+    window: only the last so many rows (0: all); scale: 1/sqrt(d) by default.
+    Returns out [hq, n_seq, d] (new if not given), and with return_lse (out, lse
+    [hq, n_seq] fp32)."""
     torch = _torch()
     if q.dim() != 3:
         _fail(2, "q must be [hq, n_seq, d]")

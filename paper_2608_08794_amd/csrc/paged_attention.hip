@@ -759,7 +759,7 @@ apack_status apack_paged_attention(int64_t n_seq, int32_t hq, const apack_heads*
   APACK_CHECK(scale == 0 || (scale >= 1e-30 && scale <= 1e30), APACK_E_ARG,
               "scale must lie in [1e-30, 1e30], or be 0 for 1/sqrt(d)");
   APACK_CHECK(n_seq == 0 || lens, APACK_E_ARG, "lens is NULL");
-  APACK_CHECK(!mask || mask_stride >= max_len, APACK_E_SHAPE, "mask_stride must be >= max_len");
+  APACK_CHECK(!mask || mask_stride >= max_len || mask_stride == 0, APACK_E_SHAPE, "mask_stride must be >= max_len, or 0");
   const size_t es = dtype_size(pages->dtype);
   Strided tq, to;
   st = check_heads(q, "q", n_seq, pages->d, es, &tq);

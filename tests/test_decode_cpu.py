@@ -502,3 +502,11 @@ def test_one_row_of_position_ids_for_all():
     # Onto the last of the ids.
     far = _heads(FAKE + (5 << 34) + 4 * 8, 4, 8, 64)
     assert _rotary(rope=rope, stride=0, q=far, qo=_heads(FAKE + (5 << 34) + 4 * 7, 4, 8, 64))[0] == 5
+
+
+def test_one_mask_for_all_sequences():
+    # A row stride of 0; refused further on, lse lying on the mask's row.
+    mask = FAKE + (18 << 34)
+    assert _attend(mask=mask, mask_stride=0, lse=mask + 60)[0] == 5
+    for stride in (1, 63, -64):
+        assert _attend(mask=mask, mask_stride=stride)[0] == 2

@@ -1062,3 +1062,18 @@ def test_position_ids_expanded_from_one_row(rows):
     table = torch.arange(rows, dtype=torch.int32, device="cuda")[:, None]
     assert torch.equal(A.apack_rotary_append(pos, rope, q, k, v, kp, vp, table, torch.full_like(pos[0], 4)), qt)
     assert torch.equal(kp[:, :, 3], kt.transpose(0, 1)) and torch.equal(vp[:, :, 3], v.transpose(0, 1))
+
+
+@pytest.mark.parametrize("dtype,pr,longest", [("bf16", 16, 700), ("f32", 16, 5000), ("bf16", 7, 300)])
+def test_mask_expanded_from_one_row(dtype, pr, longest):
+    import paper_2608_08794_amd as A
+    g = _gen(84)
+    kp, vp, table, n = _paged(g, dtype, [longest, 40, 0, longest // 2], 2, pr, 64)
+    q = _rand(g, dtype, 4, 4, 64)
+    one = torch.rand(1, longest, generator=g, device="cuda") < 0.5
+    for kind in (torch.bool, torch.uint8):
+        mask = one.to(kind).expand(4, longest)
+        o, lse = A.apack_paged_attention(q, kp, vp, table, n, longest, mask=mask, return_lse=True)
+        _check_attention(o, lse, q, kp, vp, table, n, longest, mask=mask, dtype=dtype)
+        again = A.apack_paged_attention(q, kp, vp, table, n, longest, mask=mask.contiguous())
+        np.testing.assert_array_equal(bits(o), bits(again))
