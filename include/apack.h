@@ -504,7 +504,7 @@ typedef struct apack_pages {
   void* const* k;             /* HOST array of n_layers DEVICE pointers       */
   void* const* v;             /* the same, or NULL: only K planes (moves)     */
   const int32_t* table;       /* DEVICE [sequences][table_width], or NULL     */
-  int64_t table_stride;       /* >= table_width                               */
+  int64_t table_stride;       /* >= table_width, or 0: one row for all        */
 } apack_pages;
 
 /* Bookkeeping of a pool, on the HOST: refs [n_pages] counts the tables that

@@ -26,8 +26,8 @@ apack_status check_pages(const apack_pages* p, const char* what, PoolDev* dev, S
   for (int l = 0; l < p->n_layers; ++l)
     APACK_CHECK(p->k[l] && (!p->v || p->v[l]), APACK_E_ARG, "%s: layer %d: NULL K/V pointer", what, l);
   if (p->table)
-    APACK_CHECK(p->table_width >= 0 && p->table_stride >= p->table_width, APACK_E_SHAPE,
-                "%s: table_stride must be >= table_width >= 0", what);
+    APACK_CHECK(p->table_width >= 0 && (p->table_stride >= p->table_width || p->table_stride == 0), APACK_E_SHAPE,
+                "%s: table_stride must be >= table_width >= 0, or 0", what);
   const int64_t ps = p->n_pages > 1 ? p->page_stride : 0;
   const int64_t hs = p->hkv > 1 ? p->head_stride : 0;
   const int64_t rs = p->page_rows > 1 ? p->row_stride : 0;

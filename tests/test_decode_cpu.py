@@ -510,3 +510,13 @@ def test_one_mask_for_all_sequences():
     assert _attend(mask=mask, mask_stride=0, lse=mask + 60)[0] == 5
     for stride in (1, 63, -64):
         assert _attend(mask=mask, mask_stride=stride)[0] == 2
+
+
+def test_one_table_for_all_sequences():
+    # A row stride of 0; refused further on: an output lies on the table's row, or (moved nothing) not at all.
+    table = FAKE + (9 << 34)
+    assert _attend(pages=_pages(table_stride=0), lse=table + 12)[0] == 5
+    assert _append(pages=_pages(table_stride=0), lens=table, qo=_heads(table, 4, 3, 64))[0] == 5
+    assert _compact([(0, 4, 0, 0)] * 2, pout=_pages(table_stride=0, **OUT))[0] == 0
+    for stride in (1, 3, -4):
+        assert _compact([(0, 4, 0, 0)] * 2, pout=_pages(table_stride=stride, **OUT))[0] == 2

@@ -1077,3 +1077,31 @@ def test_mask_expanded_from_one_row(dtype, pr, longest):
         _check_attention(o, lse, q, kp, vp, table, n, longest, mask=mask, dtype=dtype)
         again = A.apack_paged_attention(q, kp, vp, table, n, longest, mask=mask.contiguous())
         np.testing.assert_array_equal(bits(o), bits(again))
+
+
+def test_table_expanded_from_one_row():
+    """Several new tokens of one sequence, and moves into several parts of one."""
+    import paper_2608_08794_amd as A
+    g = _gen(85)
+    kp, vp = (_rand(g, "bf16", 8, 2, 16, 64) for _ in range(2))
+    k0, v0 = kp.clone(), vp.clone()
+    one = torch.tensor([[6, 2, 3, 7]], dtype=torch.int32, device="cuda")
+    table = one.expand(3, 4)
+    lens = torch.tensor([32, 33, 34], dtype=torch.int32, device="cuda")
+    q, k, v = (_rand(g, "bf16", h, 3, 64) for h in (4, 2, 2))
+    rope = _rope(64)
+    qt = A.apack_rotary_append(lens, rope, q, k, v, kp, vp, table, lens)
+    kt = A.apack_rotary(lens, rope, k=k)[1]
+    for s, (page, row) in enumerate([(2, 15), (3, 0), (3, 1)]):
+        k0[page, :, row], v0[page, :, row] = kt[:, s], v[:, s]
+    assert torch.equal(kp, k0) and torch.equal(vp, v0)
+    o, lse = A.apack_paged_attention(qt, kp, vp, table, lens, 64, return_lse=True)
+    _check_attention(o, lse, qt, kp, vp, table, lens, 64)
+    plane = _rand(g, "bf16", 2, 30, 64)
+    moves = [(0, 10, 20, 10), (10, 20, 35, 20), (30, 0, 0, 0)]
+    A.apack_compact_kv_pages(None, moves, [plane], [], [kp], [], table_out=table)
+    _check_move(None, moves, plane[None], kp[None], k0[None], None, table)
+    back = torch.zeros_like(plane)
+    A.apack_compact_kv_pages(torch.arange(20, 30, dtype=torch.int32, device="cuda").repeat(3),
+                             [(0, 64, 10 * i, 10) for i in range(3)], [kp], [], [back], [], table_in=table)
+    assert torch.equal(back, plane[:, :10].repeat(1, 3, 1))
