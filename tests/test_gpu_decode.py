@@ -1105,3 +1105,46 @@ def test_table_expanded_from_one_row():
     A.apack_compact_kv_pages(torch.arange(20, 30, dtype=torch.int32, device="cuda").repeat(3),
                              [(0, 64, 10 * i, 10) for i in range(3)], [kp], [], [back], [], table_in=table)
     assert torch.equal(back, plane[:, :10].repeat(1, 3, 1))
+
+
+# ---------------------------------------------------------------------------
+# Probabilities in two bf16 parts
+# ---------------------------------------------------------------------------
+
+def _one_part(q, k, v, scale):
+    """The oracle's output with each probability (of the largest) rounded once to bf16, in the products with V alone."""
+    out = np.zeros_like(q)
+    for h in range(q.shape[0]):
+        g = h // (q.shape[0] // k.shape[0])
+        x = scale * (k[g] @ q[h])
+        p = np.exp(x - x.max())
+        out[h] = torch.tensor(p).bfloat16().double().numpy() @ v[g] / p.sum()
+    return out
+
+
+@pytest.mark.parametrize("hq,hkv,d,pr", [(8, 2, 128, 16), (4, 4, 64, 5), (20, 1, 64, 32)])
+def test_paged_attention_keeps_16_bits_of_probabilities(hq, hkv, d, pr):
+    """Neighbouring rows have nearly the same K and opposite V, so that the output is small beside sum p |v| and its one
+    rounding h |o| hides little.  The first part leaves at most h p, the second h of that: 2^-16 of each probability.
+    Dropping the second part, as the oracle does here on the CPU, is out of this bound."""
+    import paper_2608_08794_amd as A
+    g = _gen(hq * d)
+    lens = [2, 4, 8, 16, 64]
+    kp, vp, table, n = _paged(g, "bf16", lens, hkv, pr, d)
+    for s, rows in enumerate(lens):
+        at = lambda j: (table[s, j // pr].long(), slice(None), j % pr)
+        for j in range(1, rows, 2):
+            kp[at(j)] = (kp[at(j - 1)].float() + 0.05 * torch.randn(hkv, d, generator=g, device="cuda")).bfloat16()
+            vp[at(j)] = -vp[at(j - 1)]
+    q = (0.25 * torch.randn(hq, len(lens), d, generator=g, device="cuda")).bfloat16()
+    scale, h = d ** -0.5, _half("bf16")
+    for bound in (64, 5000):                              # taken whole, and in shares
+        o = _f64(A.apack_paged_attention(q, kp, vp, table, n, bound))
+        for s, rows in enumerate(lens):
+            page, row = (np.array([f(j) for j in range(rows)]) for f in (lambda j: int(table[s, j // pr]), lambda j: j % pr))
+            qs, k, v = _f64(q[:, s]), *(_f64(x)[page, :, row].transpose(1, 0, 2) for x in (kp, vp))
+            want, _, w, size = OD.attention(qs, k, v, scale)
+            rel = 2 * (d + 2) * U * size[:, None] + 2 ** 7 * U + 3 * rows * U + 2.0 ** -16
+            tol = w * rel + (h + 4 * U) * np.abs(want)
+            assert (np.abs(o[:, s] - want) <= tol).all(), (rows, (np.abs(o[:, s] - want) / tol).max())
+            assert (np.abs(_one_part(qs, k, v, scale) - want) > tol).any()
