@@ -1148,3 +1148,91 @@ def test_paged_attention_keeps_16_bits_of_probabilities(hq, hkv, d, pr):
             tol = w * rel + (h + 4 * U) * np.abs(want)
             assert (np.abs(o[:, s] - want) <= tol).all(), (rows, (np.abs(o[:, s] - want) / tol).max())
             assert (np.abs(_one_part(qs, k, v, scale) - want) > tol).any()
+
+
+# ---------------------------------------------------------------------------
+# How rows are dealt to workgroups
+# ---------------------------------------------------------------------------
+
+def _dealt(hq, hkv, d, lens, max_len, window):
+    """("whole", "tiles": a share of one tile each, "own": in parts of each item's own, or "equal": equal shares of all
+    tiles; tiles a share): as the kernel decides it, from the lengths, for these sizes."""
+    import paper_2608_08794_amd as A
+    n, group = len(lens), hq // hkv
+    items = hkv * -(-group // 16)
+    span = min(window, max_len) if window else max_len
+    if span <= max(512, min(2048, 11 * n * items)):
+        return "whole", 0
+    shares = min(512, n * items * -(-span // 32))
+    up = lambda x: -(-x // 256) * 256
+    need = up(12 * n * items) + up(8 * shares * min(16, group) * (d + 4))
+    if not window:                                        # the count of shares shows in the workspace
+        assert A.apack_paged_attention_workspace(n, hq, hkv, d, max_len) == need
+    tiles = 0
+    for x in lens:
+        lo = max(0, x - window) if window else 0
+        tiles += max(1, -(-(min(x, max_len) - lo // 16 * 16) // 32)) if min(x, max_len) > lo else 1
+    total, pieces = tiles * items, n * items
+    shares = min(shares, total)
+    if total <= shares:
+        return "tiles", 1
+    if n > 1 and pieces < shares and total * pieces <= 2 * shares * (shares - pieces):
+        return "own", total / shares
+    return "equal", total / shares
+
+
+RAGGED = [(i * 2719) % 6001 if i % 7 else i % 34 for i in range(64)]   # 0 to 6000 rows; every seventh of 33 at most
+
+DEALT = [
+    # how, dtype, hq, hkv, d, page rows, window, masked, lens
+    ("equal", "bf16", 28, 4, 128, 16, 0, False, [20011]),
+    ("equal", "f32", 4, 2, 64, 16, 0, False, [20480]),
+    ("equal", "bf16", 8, 4, 128, 16, 0, False, RAGGED),
+    ("equal", "f32", 4, 4, 64, 16, 0, False, RAGGED),
+    ("equal", "bf16", 8, 4, 64, 16, 0, True, RAGGED),
+    ("equal", "bf16", 4, 4, 128, 7, 0, False, RAGGED),
+    ("equal", "f32", 8, 8, 128, 1, 0, True, [5, 700, 1301, 0, 33, 2049] * 6),
+    ("equal", "bf16", 20, 1, 64, 32, 0, False, [17000]),
+    ("equal", "bf16", 8, 4, 128, 16, 2500, False, RAGGED),
+    ("equal", "f32", 8, 8, 64, 5, 4097, True, [19999]),
+    ("own", "bf16", 8, 4, 128, 16, 4097, False, [9000, 5000, 700, 3, 0]),
+    ("own", "f32", 8, 8, 128, 16, 0, False, [3000, 2999, 640, 0]),
+    ("own", "f32", 4, 4, 64, 16, 2600, False, [6000, 5000, 2700, 40]),
+    ("own", "bf16", 8, 4, 64, 16, 0, True, [4100, 0, 3001, 555]),
+    ("own", "f32", 8, 4, 64, 48, 0, True, [4100, 0, 3001, 555]),
+    ("own", "bf16", 8, 4, 128, 5, 0, False, [3999, 17, 2500]),
+    ("own", "f32", 4, 4, 128, 7, 0, True, [3999, 17, 2500]),
+    ("own", "bf16", 6, 2, 64, 9, 4500, True, [9001, 8000, 5000]),
+    ("own", "bf16", 40, 2, 64, 16, 0, False, [3999, 0, 2500]),
+]
+
+
+@pytest.mark.parametrize("how,dtype,hq,hkv,d,pr,window,masked,lens", DEALT)
+def test_paged_attention_as_rows_are_dealt(how, dtype, hq, hkv, d, pr, window, masked, lens):
+    import paper_2608_08794_amd as A
+    longest = max(lens)
+    got, share = _dealt(hq, hkv, d, lens, longest, window)
+    assert got == how and share > 1
+    g = _gen(91)
+    kp, vp, table, n = _paged(g, dtype, lens, hkv, pr, d)
+    mask = None
+    if masked:
+        mask = torch.rand(len(lens), longest + 3, generator=g, device="cuda")[:, :longest] < 0.5
+        mask[0, :min(lens[0], longest) // 2] = False      # whole tiles and parts without a row
+    q = _rand(g, dtype, hq, len(lens), d)
+    args = dict(mask=mask, window=window)
+    o, lse = A.apack_paged_attention(q, kp, vp, table, n, longest, return_lse=True, **args)
+    _check_attention(o, lse, q, kp, vp, table, n, longest, dtype=dtype, **args)
+    again, lse2 = A.apack_paged_attention(q, kp, vp, table, n, longest, return_lse=True, **args)
+    np.testing.assert_array_equal(bits(again), bits(o))
+    np.testing.assert_array_equal(bits(lse2), bits(lse))
+
+
+def test_paged_attention_shares_hold_several_items():
+    """The equal shares above: some hold parts of three items or more, some begin or end inside one."""
+    items, tiles = 4, [max(1, -(-x // 32)) for x in RAGGED]
+    ends = np.cumsum([t for t in tiles for _ in range(items)])
+    starts = np.array([w * int(ends[-1]) // 512 for w in range(513)])
+    first, last = (np.searchsorted(ends, x, side="right") for x in (starts[:-1], starts[1:] - 1))
+    assert (last - first >= 2).any() and (last == first).any() and (last - first == 1).any()
+    assert not np.isin(starts[1:-1], ends).all()
