@@ -90,9 +90,6 @@ __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(
 
 // A value that all lanes hold, as the scalar that the compiler cannot see it is.
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
-__device__ __forceinline__ int64_t uniform(int64_t x) {
-  return (int64_t)((uint64_t)(uint32_t)uniform((int)x) | (uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32);
-}
 
 // Over the four lanes that hold a head.
 __device__ __forceinline__ float max_of_head(float x) {
@@ -114,7 +111,6 @@ template <class T> struct Elem;
 
 template <> struct Elem<uint16_t> {   // bf16 bits
   static constexpr int kRow16 = 2;    // 16-row logit tiles per step
-  static __device__ __forceinline__ float get(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
   static __device__ __forceinline__ void put(float x, uint16_t* y) {
     const __bf16 b = (__bf16)x;
     *y = __builtin_bit_cast(uint16_t, b);
@@ -122,7 +118,6 @@ template <> struct Elem<uint16_t> {   // bf16 bits
 };
 template <> struct Elem<float> {
   static constexpr int kRow16 = 1;
-  static __device__ __forceinline__ float get(float x) { return x; }
   static __device__ __forceinline__ void put(float x, float* y) { *y = x; }
 };
 
