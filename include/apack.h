@@ -416,7 +416,9 @@ apack_status apack_score_dynamics(int32_t n_seq, const apack_av_seq* seqs, apack
  *   NTK       base s^(rot_dim/(rot_dim-2)) in the place of base
  *   BY_PARTS  (1-g) f_i/s + g f_i with g = clamp((t_i - 1)/(32 - 1), 0, 1)
  *             and t_i = trained_len f_i / 2 pi turns over the trained length;
- *             the turned elements are multiplied by 0.1 ln s + 1 */
+ *             the turned elements are multiplied by 0.1 ln s + 1.  A model whose
+ *             ramp g has other ends, or runs evenly over the pairs between them,
+ *             needs frequencies of its own in freq. */
 #define APACK_ROPE_SCALE_NONE 0
 #define APACK_ROPE_SCALE_LINEAR 1
 #define APACK_ROPE_SCALE_NTK 2
@@ -466,6 +468,9 @@ typedef struct apack_heads {
  *   data and strides); otherwise it overlaps no input, no other output and not
  *   pos (APACK_E_ALIAS).  Inputs and outputs may be slices of one tensor whose
  *   elements interleave, as of a fused projection.
+ *
+ * Limits (APACK_E_UNSUPPORTED beyond): 65535 heads; fewer than 2^31 rows, and than
+ * 2^24 workgroups of one row or, of narrower ones, several.
  */
 apack_status apack_rotary(const apack_rope* rope, int64_t rows, const int32_t* pos,
                           int64_t pos_stride, apack_dtype dtype, int32_t d,
@@ -533,7 +538,9 @@ apack_status apack_pages_fork(int32_t n_pages, int32_t* refs, int32_t page_rows,
  * [n_pairs][2] array; a pair with an id outside [0, n_pages) copies nothing.
  * Pages written must be distinct and not among those read (otherwise the call
  * stays inside the pool, and their contents are unspecified).  The table of
- * `pages` is not read. */
+ * `pages` is not read.  Limit (APACK_E_UNSUPPORTED beyond): n_pairs times a page's
+ * workgroups, of 256 units of 16 bytes (of 4 or 2 where a run of rows, a stride or
+ * an address is no multiple) each, below 2^24. */
 apack_status apack_pages_copy(const apack_pages* pages, int64_t n_pairs, const int32_t* pairs,
                               void* stream);
 
@@ -562,7 +569,9 @@ typedef struct apack_move {
  * may be the same pool (the same k, v and strides) under two tables: the pages
  * written must not be among those read (otherwise the call stays inside the
  * pool, and the contents of pages written are unspecified); any other overlap
- * is APACK_E_ALIAS. */
+ * is APACK_E_ALIAS.  Limits (APACK_E_UNSUPPORTED beyond): rows below 2^31; kept
+ * rows times a row's units of 16 bytes (of 4 or 2 where a row, a stride or an
+ * address is no multiple) below 2^31 - 2^8; 65535 planes (layers x {K, V} x heads). */
 apack_status apack_compact_kv_pages(int32_t n_seq, const apack_move* seqs, const int32_t* src_rows,
                                     const apack_pages* in, const apack_pages* out, void* stream);
 
@@ -599,7 +608,8 @@ size_t apack_paged_attention_workspace(int64_t n_seq, int32_t hq, int32_t hkv, i
  * bits.  Among the others a NaN gives NaN, as does a logit of +inf, and an
  * infinity in v gives NaN or itself.
  *
- *   q, out  [hq][n_seq][d]; out overlaps neither q nor the pool.
+ *   q, out  [hq][n_seq][d]; out overlaps neither q nor the pool; every row of q
+ *           starts 16-byte aligned.
  *   lse     fp32 [hq][n_seq] out (nullable): ln sum_j exp(scale q.k_j), with
  *           which attentions over disjoint rows can be joined.
  *   pages   one layer, with v and a table of n_seq rows; d 64 or 128; every

@@ -23,8 +23,8 @@
 //
 // Measured (bf16, 28 heads over 4 of 128, pages of 16 rows), of 6.8 to 7.1 TB/s at
 // which nontemporal loads read this much alone: 64 sequences of 700 to 9454 rows
-// (0.68 GB) 107 + 5 us, 6.3 TB/s in the first kernel; one of 94028 rows (0.19 GB)
-// 34 + 4 us, 5.7 TB/s.  What is left is the launches, the first loads' chain (length,
+// (0.68 GB) 108 + 5 us, 6.2 TB/s in the first kernel; one of 94028 rows (0.19 GB)
+// 34 + 4 us, 5.6 TB/s.  What is left is the launches, the first loads' chain (length,
 // page id, row) and the join.
 #include <cmath>
 #include <cstring>

@@ -2,15 +2,16 @@
 
 Tolerances count roundings.  u is half a step of fp32 (2^-24), h half a step of
 the tensors' type.  A turned element is a c - b s with sines and cosines within
-4 u of their values (sincospi of an angle reduced in fp64), so it is within
+4 u of their values (a series, of an angle reduced in fp64), so it is within
 8 u factor (|a| + |b|) of the formula, then rounded once (h); both sides form the
 angle itself in fp64, within 2^-51 of |theta| together.
 
 A logit is a sum of d products in fp32, within (d + 2) u scale sum |q k| of the
 formula; call the largest such error e.  Probabilities then differ by a factor of
 1 + 2 e, the exponential's argument (|x - m| <= 60 where it counts, two
-roundings) adds 2^7 u, and sums over n rows n u.  With bf16 tensors each probability
-and the result are rounded once more (h each).
+roundings) adds 2^7 u, and sums over n rows n u.  With bf16 tensors the result is
+rounded once more (h); probabilities keep 16 bits, for which most tests allow one
+whole rounding (h) and the test of those bits 2^-16.
 """
 
 import numpy as np
